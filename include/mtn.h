@@ -117,7 +117,7 @@ typedef struct {
  *   K tile   [16][D]  at ((l * n_blocks + b) * Hkv + h) * 2 * 16 * D * e
  *   V^T tile [D][16]  immediately after the K tile
  *
- * K rows hold RoPE-rotated keys; the V tile is stored transposed (dimension-
+ * K rows hold RoPE-rotated keys (mtn_pool_set_rope names the forms); the V tile is stored transposed (dimension-
  * major) so that consecutive tokens of one dimension are adjacent.
  *
  * MTN_FP8_E4M3 (D = 128): each (l, b, h) region is 4224 bytes at
@@ -148,6 +148,48 @@ mtn_status mtn_pool_create(const mtn_pool_config *cfg, void *kv_dev, size_t kv_b
 /* Frees the library's host and device state (not kv_dev).  Synchronises the
  * device first.  NULL is accepted.                                            */
 void mtn_pool_destroy(mtn_pool *pool);
+
+/*
+ * Rotary positions of a pool.  A pool is created with whole rotate-half rows at
+ * the frequencies theta^(-2i/D); mtn_pool_set_rope replaces that for every
+ * later append and query, while no open session holds tokens
+ * (MTN_ERR_BAD_STATE otherwise, or while a plan is open).  With rd =
+ * rotary_dim, pair i < rd/2 of a row at position p is turned by p * f_i
+ * (angle in fp64) and scaled by m:
+ *   y_a = m (x_a cos - x_b sin),   y_b = m (x_b cos + x_a sin)
+ * where (a, b) is (i, i + rd/2) for MTN_ROPE_HALF and (2i, 2i + 1) for
+ * MTN_ROPE_INTERLEAVED; elements rd .. D - 1 are left as they are.
+ *   NONE    f_i = theta^(-2i/rd)
+ *   LINEAR  f_i = theta^(-2i/rd) / factor              (positions divided)
+ *   BASE    theta replaced by theta * factor^(rd/(rd-2))
+ *   YARN    f_i = theta^(-2i/rd) * ((1 - r_i) + r_i / factor), r_i = clamp((i -
+ *           lo) / max(hi - lo, 0.001), 0, 1), lo = max(floor(c(beta_fast)), 0),
+ *           hi = min(ceil(c(beta_slow)), rd - 1), c(b) = rd ln(original_len /
+ *           (2 pi b)) / (2 ln theta): pairs that turn often over the trained
+ *           length keep their frequency, slow ones are divided
+ * m is `magnitude`; 0 selects 0.1 ln(factor) + 1 with YARN and 1 otherwise.
+ * Stored key rows: pair i lies in dims i and i + D/2 of the K tile in every
+ * form (pairs past rd/2 hold the elements left as they are).
+ */
+enum { MTN_ROPE_HALF = 0, MTN_ROPE_INTERLEAVED = 1 };
+enum { MTN_ROPE_SCALE_NONE = 0, MTN_ROPE_SCALE_LINEAR = 1, MTN_ROPE_SCALE_BASE = 2,
+       MTN_ROPE_SCALE_YARN = 3 };
+
+typedef struct {
+    int32_t layout;        /* MTN_ROPE_HALF | MTN_ROPE_INTERLEAVED             */
+    int32_t rotary_dim;    /* 0 = head_dim, else a multiple of 16 (otherwise
+                              MTN_ERR_UNSUPPORTED) up to head_dim              */
+    int32_t scaling;       /* MTN_ROPE_SCALE_*                                 */
+    int32_t original_len;  /* YARN: trained context in tokens, >= 1            */
+    double  factor;        /* scaling: >= 1, finite (ignored with NONE)        */
+    double  beta_fast;     /* YARN: turns over the trained context; 0 = 32     */
+    double  beta_slow;     /* YARN: 0 = 1; 0 < beta_slow < beta_fast           */
+    double  magnitude;     /* >= 0, finite; 0 = by scaling                     */
+} mtn_rope_config;
+
+/* Synchronises the stream of the pool's previous plan.  An all-zero config is
+ * the form that a pool is created with.                                       */
+mtn_status mtn_pool_set_rope(mtn_pool *pool, const mtn_rope_config *rope);
 
 /* Open a session: lowest free session id.  Windowed pools reserve the
  * session's whole bounded footprint, ceil(S/16) sink blocks plus R/16 ring
@@ -204,8 +246,8 @@ mtn_status mtn_plan_abort(mtn_pool *pool);
  * the absolute position they were appended at; App. A: positions behind the
  * window are not retained, sink blocks stay).
  * k, v: device, [T][Hkv][D] in kv_dtype, T = total planned tokens, packed in
- * plan order.  Each key row is rotated (rotate-half RoPE at its absolute
- * position, angle computed in fp64) and written with its value into the
+ * plan order.  Each key row is rotated (RoPE at its absolute position,
+ * rotate-half unless mtn_pool_set_rope says otherwise, angle computed in fp64) and written with its value into the
  * token's slot of layer `layer`, overwriting whatever position left the window
  * there (eviction is slot reuse).  Errors: MTN_ERR_BAD_STATE (no open plan,
  * host-only pool), MTN_ERR_INVALID_ARG (layer, null pointer, stream other

@@ -131,6 +131,44 @@ def rope_rotate(x: np.ndarray, pos: int, theta: float) -> np.ndarray:
     return np.concatenate([lo * c - hi * s, hi * c + lo * s], axis=-1)
 
 
+def rope_form(x: np.ndarray, pos: int, theta: float, *, layout: str = "half",
+              rotary_dim: int = 0, scaling: str = "none", factor: float = 1.0,
+              original_len: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0,
+              magnitude: float = 0.0) -> np.ndarray:
+    """RoPE of ``x[..., D]`` at ``pos`` in one of the forms a pool can be set to.
+
+    Each pair of elements is one complex number x_a + i x_b, multiplied by
+    m exp(i pos f); pairs are neighbours ("interleaved") or rd/2 apart ("half");
+    elements from rd = rotary_dim on stay.  Frequencies: "linear" divides them
+    all by ``factor``; "base" raises theta; "yarn" divides only those that make
+    fewer than beta_slow turns over original_len, none above beta_fast, ramped
+    in between by pair index, with m = 0.1 ln(factor) + 1.
+    """
+    x = np.asarray(x, dtype=np.float64)
+    rd = rotary_dim or x.shape[-1]
+    a = np.arange(0, rd, 2) if layout == "interleaved" else np.arange(rd // 2)
+    b = a + (1 if layout == "interleaved" else rd // 2)
+    i = np.arange(rd // 2, dtype=np.float64)
+    if scaling == "base":
+        theta = theta * factor ** (rd / (rd - 2.0))
+    f = np.float64(theta) ** (-i / (rd / 2.0))
+    m = magnitude or 1.0
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "yarn":
+        # pair index at which the turns over original_len equal beta
+        lo, hi = (rd / 2.0 * np.log(original_len / (2.0 * np.pi * beta)) / np.log(theta)
+                  for beta in (beta_fast, beta_slow))
+        lo, hi = max(np.floor(lo), 0.0), min(np.ceil(hi), rd - 1.0)
+        slow = np.clip((i - lo) / max(hi - lo, 1e-3), 0.0, 1.0)
+        f = (1.0 - slow) * f + slow * (f / factor)
+        m = magnitude or 0.1 * math.log(factor) + 1.0
+    z = (x[..., a] + 1j * x[..., b]) * (m * np.exp(1j * (np.float64(pos) * f)))
+    y = x.copy()
+    y[..., a], y[..., b] = z.real, z.imag
+    return y
+
+
 # ---------------------------------------------------------------------------
 # One query row against an explicit key set
 # ---------------------------------------------------------------------------
@@ -167,7 +205,7 @@ class OracleSession:
                  n_sink: int, window: Optional[int], theta: float = 10000.0,
                  scale: Optional[float] = None, n_layers: int = 1,
                  literal_window: bool = False, check_psum: bool = True,
-                 kv_quant: Optional[str] = None):
+                 kv_quant: Optional[str] = None, rope: Optional[dict] = None):
         if n_q_heads % n_kv_heads:
             raise ValueError("n_q_heads must be a multiple of n_kv_heads")
         self.hq, self.hkv, self.d = n_q_heads, n_kv_heads, head_dim
@@ -175,6 +213,7 @@ class OracleSession:
         self.n_sink = 0 if window is None else n_sink
         self.window = window
         self.theta = theta
+        self.rope = rope  # rope_form's keywords, or None for whole rotate-half rows
         self.scale = 1.0 / math.sqrt(head_dim) if scale is None else scale
         self.n_layers = n_layers
         self.literal = literal_window
@@ -188,6 +227,11 @@ class OracleSession:
         self._pending: Optional[int] = None
         self._done = set()
         self.last_evicted = (0, 0)
+
+    def _rotate(self, x: np.ndarray, pos: int) -> np.ndarray:
+        if self.rope is None:
+            return rope_rotate(x, pos, self.theta)
+        return rope_form(x, pos, self.theta, **self.rope)
 
     # -- frame structure -------------------------------------------------
     def begin(self, n_tok: int) -> List[int]:
@@ -217,7 +261,7 @@ class OracleSession:
         # Insert every chunk token first: each query then sees the earlier
         # tokens of its own chunk (causal inside the chunk).
         for i in range(c):
-            kr = rope_rotate(k[i], base + i, self.theta)
+            kr = self._rotate(k[i], base + i)
             vi = v[i].copy()
             if self.kv_quant == "fp8_e4m3":
                 # the cache holds what the quantized pool returns: each
@@ -238,7 +282,7 @@ class OracleSession:
             assert not missing, f"visible positions not resident: {missing[:5]}"
             kmat = np.stack([st[p][0] for p in vis])  # [n, Hkv, D]
             vmat = np.stack([st[p][1] for p in vis])
-            qr = rope_rotate(q[i], t, self.theta)     # [Hq, D]
+            qr = self._rotate(q[i], t)                # [Hq, D]
             for h in range(self.hq):
                 kv = h // self.g
                 o, l, psum = attend_row(qr[h], kmat[:, kv, :], vmat[:, kv, :],

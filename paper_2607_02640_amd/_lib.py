@@ -35,12 +35,16 @@ DTYPES = {"f32": (MTN_F32, MTN_F32), "bf16": (MTN_BF16, MTN_BF16),
           "fp8": (MTN_FP8_E4M3, MTN_BF16)}
 MTN_WINDOW_UNBOUNDED = -1
 MTN_POOL_HOST_ONLY = 1
+# rotary forms of Pool.set_rope
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "yarn": 3}
 
 # every symbol include/mtn.h declares
 EXPORTS = [
     "mtn_pool_required_bytes", "mtn_pool_create", "mtn_pool_destroy",
     "mtn_session_open", "mtn_session_close", "mtn_plan_begin", "mtn_plan_commit",
     "mtn_plan_abort",
+    "mtn_pool_set_rope",
     "mtn_frame_append_kv", "mtn_attend_chunk_prefill", "mtn_attend_decode",
     "mtn_attend_decode_append", "mtn_attend_decode_noalloc",
     "mtn_frame_step", "mtn_pool_stats", "mtn_session_info", "mtn_session_block_table",
@@ -60,6 +64,14 @@ class PoolConfig(C.Structure):
         ("max_len", C.c_int32), ("n_blocks", C.c_int64), ("kv_dtype", C.c_int32),
         ("io_dtype", C.c_int32), ("rope_theta", C.c_double), ("softmax_scale", C.c_float),
         ("flags", C.c_uint32),
+    ]
+
+
+class RopeConfig(C.Structure):
+    _fields_ = [
+        ("layout", C.c_int32), ("rotary_dim", C.c_int32), ("scaling", C.c_int32),
+        ("original_len", C.c_int32), ("factor", C.c_double), ("beta_fast", C.c_double),
+        ("beta_slow", C.c_double), ("magnitude", C.c_double),
     ]
 
 
@@ -119,6 +131,7 @@ def load() -> C.CDLL:
         "mtn_pool_required_bytes": (i32, [C.POINTER(PoolConfig), C.POINTER(C.c_size_t)]),
         "mtn_pool_create": (i32, [C.POINTER(PoolConfig), vp, C.c_size_t, vp, C.POINTER(vp)]),
         "mtn_pool_destroy": (None, [vp]),
+        "mtn_pool_set_rope": (i32, [vp, C.POINTER(RopeConfig)]),
         "mtn_session_open": (i32, [vp, P32]),
         "mtn_session_close": (i32, [vp, i32]),
         "mtn_plan_begin": (i32, [vp, i32, P32, P32, vp]),
@@ -274,6 +287,14 @@ class Pool:
 
     def plan_abort(self) -> None:
         self._check(self.lib.mtn_plan_abort(self.h), "plan_abort")
+
+    def set_rope(self, *, layout="half", rotary_dim=0, scaling="none", factor=1.0, original_len=0,
+                 beta_fast=0.0, beta_slow=0.0, magnitude=0.0) -> None:
+        """Rotary positions of later appends and queries (mtn_pool_set_rope): layout
+        "half" or "interleaved", scaling "none", "linear", "base" or "yarn"."""
+        cfg = RopeConfig(ROPE_LAYOUTS[layout], rotary_dim, ROPE_SCALINGS[scaling], original_len,
+                         factor, beta_fast, beta_slow, magnitude)
+        self._check(self.lib.mtn_pool_set_rope(self.h, C.byref(cfg)), "set_rope")
 
     def set_decode_kernel(self, kind: int) -> None:
         """0 = by shape, 1 = vector kernel, 2 = matrix-core kernel."""

@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -58,15 +59,17 @@ def _run(cmd, verbose):
 def build(verbose: bool = False, out: str = LIB, defines=()) -> str:
     """Compile every source for gfx950 and link libmtn.so next to this file
     (or at ``out``, with extra ``-D`` ``defines`` for tuning variants)."""
-    objs = []
     tag = "_".join("".join(ch for ch in d if ch.isalnum()) for d in defines)
     bdir = os.path.join(ROOT, "_build", tag) if tag else os.path.join(ROOT, "_build")
     os.makedirs(bdir, exist_ok=True)
-    for src in SOURCES:
+
+    def compile_one(src):
         obj = os.path.join(bdir, src + ".o")
         _run([HIPCC, *compile_flags(src), *[f"-D{d}" for d in defines], "-c",
               os.path.join(CSRC, src), "-o", obj], verbose)
-        objs.append(obj)
+        return obj
+    with ThreadPoolExecutor(len(SOURCES)) as ex:
+        objs = list(ex.map(compile_one, SOURCES))
     tmp = out + ".tmp"
     _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp], verbose)
     os.replace(tmp, out)

@@ -130,6 +130,66 @@ __device__ __forceinline__ void wave_sync() {
 }
 
 // ---------------------------------------------------------------------------
+// rotation pairs of an input row (see PoolGeom)
+// ---------------------------------------------------------------------------
+// The kernels that rotate are built twice: RF false for whole rotate-half rows,
+// whose offsets are constants, RF true for every other form.  With one
+// instance that tests the form, a lone session's frame of 768 decode
+// launches took 9.76 ms instead of 9.68, two-layer fp32 frames 349 us instead
+// of 340.
+inline bool rope_form(const PoolGeom &g) { return g.rope_il || g.rope_half != g.d / 2; }
+// Elements of an input row that become dims i and i + D/2 (i < D/2)
+template <bool RF>
+__device__ __forceinline__ int rope_a(const PoolGeom &g, int i) {
+    if constexpr (!RF) return i;
+    return g.rope_il ? 2 * i : i < g.rope_half ? i : i + g.rope_half;
+}
+template <bool RF>
+__device__ __forceinline__ int rope_b(const PoolGeom &g, int i, int D) {
+    if constexpr (!RF) return i + D / 2;
+    return g.rope_il ? 2 * i + 1 : i < g.rope_half ? i + g.rope_half : i + D / 2;
+}
+// The same for a vector of n dims d0 .. d0 + n - 1 (n divides d0, 8 and
+// rope_half) and its partners: the offsets of two vectors that hold them,
+// which rope_split then sorts.
+struct RopeSrc {
+    int x, y;
+};
+template <bool RF>
+__device__ __forceinline__ RopeSrc rope_src(const PoolGeom &g, int d0, int n, int D) {
+    if constexpr (!RF) return RopeSrc{d0, d0 ^ (D / 2)};
+    const int i0 = d0 & (D / 2 - 1);
+    if (g.rope_il) return RopeSrc{2 * i0, 2 * i0 + n};
+    const int a = i0 < g.rope_half ? i0 : i0 + g.rope_half;
+    const int b = i0 < g.rope_half ? i0 + g.rope_half : i0 + D / 2;
+    return d0 < D / 2 ? RopeSrc{a, b} : RopeSrc{b, a};
+}
+// Interleaved pairs as loaded (x, then y, in memory order) -> the dims
+// themselves in x and their partners in y; upper: the dims are >= D/2.  The
+// bf16 forms pick halves with one byte permutation per result.
+__device__ __forceinline__ void rope_split(uint32_t &x, uint32_t &y, bool upper) {
+    const uint32_t sx = upper ? 0x07060302u : 0x05040100u;
+    const uint32_t u = x, w = y;
+    x = __builtin_amdgcn_perm(w, u, sx);
+    y = __builtin_amdgcn_perm(w, u, sx ^ 0x02020202u);
+}
+__device__ __forceinline__ void rope_split(uint4 &x, uint4 &y, bool upper) {
+    const uint32_t sx = upper ? 0x07060302u : 0x05040100u, sy = sx ^ 0x02020202u;
+    const uint4 u = x, w = y;
+    x = make_uint4(__builtin_amdgcn_perm(u.y, u.x, sx), __builtin_amdgcn_perm(u.w, u.z, sx),
+                   __builtin_amdgcn_perm(w.y, w.x, sx), __builtin_amdgcn_perm(w.w, w.z, sx));
+    y = make_uint4(__builtin_amdgcn_perm(u.y, u.x, sy), __builtin_amdgcn_perm(u.w, u.z, sy),
+                   __builtin_amdgcn_perm(w.y, w.x, sy), __builtin_amdgcn_perm(w.w, w.z, sy));
+}
+// ... of four fp32 dims held as bits
+__device__ __forceinline__ void rope_split_f32(uint4 &x, uint4 &y, bool upper) {
+    const uint4 u = x, w = y;
+    const uint4 ev = make_uint4(u.x, u.z, w.x, w.z), od = make_uint4(u.y, u.w, w.y, w.w);
+    x = upper ? od : ev;
+    y = upper ? ev : od;
+}
+
+// ---------------------------------------------------------------------------
 // visible-range geometry of one query (sinks first, then the ring run)
 // ---------------------------------------------------------------------------
 struct VisRange {

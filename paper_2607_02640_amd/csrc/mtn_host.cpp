@@ -122,7 +122,9 @@ struct mtn_pool {
     int32_t *d_table = nullptr;
     int32_t *d_meta = nullptr;     // packed plan metadata
     float2 *d_rope = nullptr;      // [max_tok][D/2]
-    double *d_inv_freq = nullptr;  // [D/2]
+    double *d_inv_freq = nullptr;  // [2][D/2]: radians per position, then the factor on (cos, sin)
+    int32_t rope_half = 0;         // rotated pairs (rotary_dim / 2)
+    bool rope_il = false;          // pairs are neighbouring elements
     float *d_part = nullptr;       // decode split partials
     float *d_scratch = nullptr;    // the static partials workspace (not owned)
     size_t scratch_floats = 0;
@@ -713,8 +715,66 @@ PoolGeom geom(const mtn_pool *P) {
     g.n_sink_blocks = P->nsb;
     g.hq = P->cfg.n_q_heads;
     g.hkv = P->cfg.n_kv_heads;
-    g.d = P->cfg.head_dim;
+    g.d = (uint16_t)P->cfg.head_dim;
+    g.rope_half = (uint8_t)P->rope_half;
+    g.rope_il = P->rope_il ? 1 : 0;
     return g;
+}
+
+mtn_status check_rope(const mtn_pool_config &c, const mtn_rope_config &r) {
+    if (r.layout != MTN_ROPE_HALF && r.layout != MTN_ROPE_INTERLEAVED) return MTN_ERR_INVALID_ARG;
+    if (r.rotary_dim < 0 || r.rotary_dim > c.head_dim) return MTN_ERR_INVALID_ARG;
+    if (r.rotary_dim % 16) return MTN_ERR_UNSUPPORTED;
+    if (r.scaling < MTN_ROPE_SCALE_NONE || r.scaling > MTN_ROPE_SCALE_YARN) return MTN_ERR_INVALID_ARG;
+    // (written so that NaN fails)
+    if (!(r.magnitude >= 0.0) || !std::isfinite(r.magnitude)) return MTN_ERR_INVALID_ARG;
+    if (r.scaling != MTN_ROPE_SCALE_NONE && (!(r.factor >= 1.0) || !std::isfinite(r.factor)))
+        return MTN_ERR_INVALID_ARG;
+    const double rd = r.rotary_dim ? r.rotary_dim : c.head_dim;
+    if (r.scaling == MTN_ROPE_SCALE_BASE &&
+        !std::isfinite(c.rope_theta * std::pow(r.factor, rd / (rd - 2.0))))
+        return MTN_ERR_INVALID_ARG;
+    if (r.scaling == MTN_ROPE_SCALE_YARN) {
+        const double fast = r.beta_fast == 0.0 ? 32.0 : r.beta_fast;
+        const double slow = r.beta_slow == 0.0 ? 1.0 : r.beta_slow;
+        if (r.original_len < 1) return MTN_ERR_INVALID_ARG;
+        if (!(slow > 0.0) || !(fast > slow) || !std::isfinite(fast)) return MTN_ERR_INVALID_ARG;
+    }
+    return MTN_OK;
+}
+
+// Frequencies (radians per position) and factors on (cos, sin) of the D/2
+// pairs of a row, [2][D/2].  Pairs past the rotated ones: 0 and 1, which
+// leaves their elements as they are.
+std::vector<double> rope_table(const mtn_pool_config &c, const mtn_rope_config &r) {
+    const int half = c.head_dim / 2;
+    const double rd = r.rotary_dim ? r.rotary_dim : c.head_dim;
+    std::vector<double> t(2 * (size_t)half, 0.0);
+    double base = c.rope_theta, mag = r.magnitude > 0.0 ? r.magnitude : 1.0;
+    if (r.scaling == MTN_ROPE_SCALE_BASE) base *= std::pow(r.factor, rd / (rd - 2.0));
+    // the pair that makes `turns` turns over the trained length
+    auto pair_of = [&](double turns) {
+        return rd * std::log(r.original_len / (turns * 6.283185307179586476925)) / (2.0 * std::log(base));
+    };
+    double lo = 0.0, hi = 1.0;
+    if (r.scaling == MTN_ROPE_SCALE_YARN) {
+        lo = std::max(std::floor(pair_of(r.beta_fast == 0.0 ? 32.0 : r.beta_fast)), 0.0);
+        hi = std::min(std::ceil(pair_of(r.beta_slow == 0.0 ? 1.0 : r.beta_slow)), rd - 1.0);
+        if (r.magnitude == 0.0) mag = 0.1 * std::log(r.factor) + 1.0;
+    }
+    for (int i = 0; i < half; ++i) {
+        t[(size_t)half + i] = 1.0;
+        if (i >= rd / 2) continue;
+        double f = std::pow(base, -2.0 * i / rd);
+        if (r.scaling == MTN_ROPE_SCALE_LINEAR) f /= r.factor;
+        if (r.scaling == MTN_ROPE_SCALE_YARN) {
+            const double ramp = std::min(std::max((i - lo) / std::max(hi - lo, 0.001), 0.0), 1.0);
+            f = f * (1.0 - ramp) + f / r.factor * ramp;
+        }
+        t[i] = f;
+        t[(size_t)half + i] = mag;
+    }
+    return t;
 }
 
 mtn_status check_call(mtn_pool *P, int32_t layer, void *stream) {
@@ -1100,6 +1160,7 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
     P->layer_stride = P->block_stride * cfg->n_blocks;
     P->scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale
                                         : (float)(1.0 / std::sqrt((double)cfg->head_dim));
+    P->rope_half = cfg->head_dim / 2;
     P->kv = (uint8_t *)kv_dev;
     P->table.assign((size_t)cfg->max_sessions * P->row_len, -1);
     P->is_open.assign((size_t)cfg->max_sessions, 0);
@@ -1152,12 +1213,10 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
         size_t half = (size_t)cfg->head_dim / 2;
         if ((e = hipMalloc(&P->d_rope, sizeof(float2) * half * (size_t)P->max_tok)) != hipSuccess)
             return bail(e, "rope");
-        std::vector<double> inv(half);
-        for (size_t i = 0; i < half; ++i)
-            inv[i] = std::pow(cfg->rope_theta, -2.0 * (double)i / (double)cfg->head_dim);
-        if ((e = hipMalloc(&P->d_inv_freq, sizeof(double) * half)) != hipSuccess)
+        const std::vector<double> inv = rope_table(*cfg, mtn_rope_config{});
+        if ((e = hipMalloc(&P->d_inv_freq, sizeof(double) * inv.size())) != hipSuccess)
             return bail(e, "inv_freq");
-        if ((e = hipMemcpy(P->d_inv_freq, inv.data(), sizeof(double) * half,
+        if ((e = hipMemcpy(P->d_inv_freq, inv.data(), sizeof(double) * inv.size(),
                            hipMemcpyHostToDevice)) != hipSuccess)
             return bail(e, "inv_freq upload");
         int dev = 0, n_cu = 0;
@@ -1228,6 +1287,27 @@ void mtn_pool_destroy(mtn_pool *P) {
         if (P->order_ev) (void)hipEventDestroy(P->order_ev);
     }
     delete P;
+}
+
+mtn_status mtn_pool_set_rope(mtn_pool *P, const mtn_rope_config *rope) {
+    return guarded(P, [&]() -> mtn_status {
+        if (!P || !rope) return fail(P, MTN_ERR_INVALID_ARG, "null argument");
+        if (P->plan_open) return fail(P, MTN_ERR_BAD_STATE, "plan open");
+        for (int32_t sid = 0; sid < P->cfg.max_sessions; ++sid)
+            if (P->is_open[sid] && P->len[sid])
+                return fail(P, MTN_ERR_BAD_STATE, "a session holds keys rotated the present way");
+        const mtn_status st = check_rope(P->cfg, *rope);
+        if (st) return fail(P, st, "bad rotary config");
+        const std::vector<double> t = rope_table(P->cfg, *rope);
+        if (!P->host_only) {
+            // plans of closed sessions may still read the table
+            if (P->have_last_stream) HIP_TRY(P, hipStreamSynchronize((hipStream_t)P->last_stream));
+            HIP_TRY(P, hipMemcpy(P->d_inv_freq, t.data(), sizeof(double) * t.size(), hipMemcpyHostToDevice));
+        }
+        P->rope_half = (rope->rotary_dim ? rope->rotary_dim : P->cfg.head_dim) / 2;
+        P->rope_il = rope->layout == MTN_ROPE_INTERLEAVED;
+        return MTN_OK;
+    });
 }
 
 mtn_status mtn_session_open(mtn_pool *P, int32_t *sid_out) {

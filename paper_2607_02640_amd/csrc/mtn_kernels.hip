@@ -47,7 +47,8 @@ __global__ void k_plan_apply(const uint4 *__restrict__ src, uint4 *__restrict__ 
         double a = (double)tok_pos[t] * inv_freq[f];
         double sn, cs;
         sincos(a, &sn, &cs);
-        rope[j] = make_float2((float)cs, (float)sn);
+        const double mag = inv_freq[half_d + f];
+        rope[j] = make_float2((float)(cs * mag), (float)(sn * mag));
     }
 }
 
@@ -63,7 +64,7 @@ __global__ void k_plan_apply(const uint4 *__restrict__ src, uint4 *__restrict__ 
 // [off0, off0 + len) in memory order: whole row segments instead of one
 // 2-byte element per 32 bytes.
 constexpr int kAppendWaves = 4;
-template <typename T>
+template <typename T, bool RF>
 __global__ __launch_bounds__(64 * kAppendWaves) void k_append(PoolGeom g, PlanView p, int32_t layer,
                                                             const T *__restrict__ k,
                                                             const T *__restrict__ v,
@@ -91,7 +92,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_append(PoolGeom g, PlanVi
         T *kd = K + (off0 + j) * D;
         for (int i = lane; i < half; i += 64) {
             const float2 cs = p.rope[(int64_t)t * half + i];
-            const float x0 = to_f32(kr[i]), x1 = to_f32(kr[i + half]);
+            const float x0 = to_f32(kr[rope_a<RF>(g, i)]), x1 = to_f32(kr[rope_b<RF>(g, i, D)]);
             kd[i] = from_f32<T>(fmaf(x0, cs.x, -x1 * cs.y));
             kd[i + half] = from_f32<T>(fmaf(x1, cs.x, x0 * cs.y));
             tr[i * kBlock + j] = vr[i];
@@ -167,7 +168,7 @@ struct DecodeShape {
 // them.  At the end the groups' (max, sum, acc) are merged through LDS by
 // log-sum-exp, so several waves per SIMD stream one unit with no second
 // launch.
-template <typename T, int D, int G, int WPU, int NG, int NBUF>
+template <typename T, int D, int G, int WPU, int NG, int NBUF, bool RF>
 __global__ __launch_bounds__(64 * WPU * NG) void k_attn_valu(AttnArgs a) {
     using L = Lay<T, D>;
     constexpr int HW = G / WPU;                     // heads per wave
@@ -290,14 +291,31 @@ __global__ __launch_bounds__(64 * WPU * NG) void k_attn_valu(AttnArgs a) {
         };
 #pragma unroll
         for (int vq = 0; vq < NVQ; ++vq) {
+            // the vector's elements of row r and their partners, as floats
+            auto load_pair = [&](const T *r, float *xs, float *ys) __attribute__((always_inline)) {
+                if constexpr (RF) {
+                    const RopeSrc o = rope_src<RF>(g, d0 + vq * EPV, EPV, D);
+                    uint4 x = *(const uint4 *)(r + o.x), y = *(const uint4 *)(r + o.y);
+                    if (g.rope_il) {
+                        if constexpr (sizeof(T) == 2)
+                            rope_split(x, y, qtr >= 2);
+                        else
+                            rope_split_f32(x, y, qtr >= 2);
+                    }
+                    unpack(x, xs);
+                    unpack(y, ys);
+                } else {
+                    unpack(((const uint4 *)(r + d0))[vq], xs);
+                    unpack(((const uint4 *)(r + dp))[vq], ys);
+                }
+            };
             float2 cs[EPV];
 #pragma unroll
             for (int e = 0; e < EPV; ++e) cs[e] = rp[vq * EPV + e];
             uint32_t kv4[4];  // the newest key's rotated vector (stored layout)
             if (own_new) {
                 float xs[EPV], ys[EPV];
-                unpack(((const uint4 *)(kb + d0))[vq], xs);
-                unpack(((const uint4 *)(kb + dp))[vq], ys);
+                load_pair(kb, xs, ys);
 #pragma unroll
                 for (int e = 0; e < EPV; e += 2) {
                     const float k0 = fmaf(xs[e], cs[e].x, sgn * ys[e] * cs[e].y);
@@ -315,8 +333,7 @@ __global__ __launch_bounds__(64 * WPU * NG) void k_attn_valu(AttnArgs a) {
 #pragma unroll
             for (int h = 0; h < HW; ++h) {
                 float xs[EPV], ys[EPV];
-                unpack(((const uint4 *)(qb + (int64_t)h * D + d0))[vq], xs);
-                unpack(((const uint4 *)(qb + (int64_t)h * D + dp))[vq], ys);
+                load_pair(qb + (int64_t)h * D, xs, ys);
 #pragma unroll
                 for (int e = 0; e < EPV; e += 2) {
                     const int i = vq * EPV + e;
@@ -907,7 +924,7 @@ __device__ __forceinline__ void f8_stage_to_bf16(const uint8_t *src, uint8_t *ds
 // regions (per block four 1 KiB DMA instructions plus the 32 exponent
 // bytes), and every stage is converted into one of two bf16 stage buffers (a
 // second barrier) before the same MFMA stage body runs on it.
-template <int D, int G, bool F8>
+template <int D, int G, bool F8, bool RF>
 __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
     using Lds = PfLds<D>;
     static_assert(D == 128 || (D == 64 && !F8), "head dims with a stage layout");
@@ -1127,8 +1144,8 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             const int64_t ri = ((int64_t)(row_t0 + j) * g.hkv + kvh) * D;
             const uint16_t *kr = (const uint16_t *)a.k_new + ri;
             const uint16_t *vr = (const uint16_t *)a.v_new + ri;
-            b.k0[u] = kr[lane];
-            b.k1[u] = kr[lane + 64];
+            b.k0[u] = kr[rope_a<RF>(g, lane)];
+            b.k1[u] = kr[rope_b<RF>(g, lane, D)];
             b.v0[u] = vr[lane];
             b.v1[u] = vr[lane + 64];
             b.cs[u] = a.p.rope[(int64_t)t * (D / 2) + lane];
@@ -1258,9 +1275,9 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             const float2 *rp = a.p.rope + (int64_t)t * (D / 2);
 #pragma unroll
             for (int s = 0; s < ND; ++s) {
-                const int d0 = s * 32 + 8 * lg;
-                qx[i][s] = *(const uint4 *)(qh + d0);
-                qy[i][s] = *(const uint4 *)(qh + (d0 ^ (D / 2)));
+                const RopeSrc o = rope_src<RF>(g, s * 32 + 8 * lg, 8, D);
+                qx[i][s] = *(const uint4 *)(qh + o.x);
+                qy[i][s] = *(const uint4 *)(qh + o.y);
             }
 #pragma unroll
             for (int h2 = 0; h2 < ND / 2; ++h2)
@@ -1277,6 +1294,12 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             for (int st = 0; st < kPfEarly; ++st) issue_block(st, phys(2 * st + db));
         }
         __builtin_amdgcn_sched_barrier(0);
+        if (RF && g.rope_il) {
+#pragma unroll
+            for (int i = 0; i < kPfTpw; ++i)
+#pragma unroll
+                for (int s = 0; s < ND; ++s) rope_split(qx[i][s], qy[i][s], s >= ND / 2);
+        }
 #pragma unroll
         for (int i = 0; i < kPfTpw; ++i) {
 #pragma unroll
@@ -1794,8 +1817,11 @@ hipError_t launch_valu_t(const AttnArgs &a, hipStream_t s) {
     int64_t units = (int64_t)a.p.n_tok * a.g.hkv * a.n_split;
     if (units == 0) return hipSuccess;
     if (units > INT32_MAX) return hipErrorInvalidValue;  // one grid dimension, 32-bit unit index
-    hipLaunchKernelGGL((k_attn_valu<T, D, G, DS::WPU, DS::NG, DS::NBUF>), dim3((unsigned)units),
-                       dim3(64 * DS::WPU * DS::NG), 0, s, a);
+    const dim3 grid((unsigned)units), block(64 * DS::WPU * DS::NG);
+    if (rope_form(a.g))
+        hipLaunchKernelGGL((k_attn_valu<T, D, G, DS::WPU, DS::NG, DS::NBUF, true>), grid, block, 0, s, a);
+    else
+        hipLaunchKernelGGL((k_attn_valu<T, D, G, DS::WPU, DS::NG, DS::NBUF, false>), grid, block, 0, s, a);
     return hipGetLastError();
 }
 
@@ -1815,7 +1841,7 @@ int resident_t() {
     using DS = DecodeShape<G>;
     int n = 0;
     if (hipOccupancyMaxActiveBlocksPerMultiprocessor(
-            &n, k_attn_valu<T, D, G, DS::WPU, DS::NG, DS::NBUF>, 64 * DS::WPU * DS::NG, 0) !=
+            &n, k_attn_valu<T, D, G, DS::WPU, DS::NG, DS::NBUF, false>, 64 * DS::WPU * DS::NG, 0) !=
         hipSuccess)
         return 1;
     return n > 0 ? n : 1;
@@ -1876,12 +1902,15 @@ hipError_t launch_append(int dtype, const PoolGeom &g, const PlanView &p, int32_
     if (groups == 0) return hipSuccess;
     if (groups > INT32_MAX) return hipErrorInvalidValue;
     const unsigned grid = (unsigned)groups;
+    auto launch = [&](auto elt, auto rf) {
+        using T = decltype(elt);
+        hipLaunchKernelGGL((k_append<T, decltype(rf)::value>), dim3(grid), dim3(64 * kAppendWaves), 0, s,
+                           g, p, layer, (const T *)k, (const T *)v, run_tok0, run_len);
+    };
     if (dtype == 1)
-        hipLaunchKernelGGL(k_append<bf16_t>, dim3(grid), dim3(64 * kAppendWaves), 0, s, g, p, layer,
-                           (const bf16_t *)k, (const bf16_t *)v, run_tok0, run_len);
+        rope_form(g) ? launch(bf16_t{}, std::true_type{}) : launch(bf16_t{}, std::false_type{});
     else
-        hipLaunchKernelGGL(k_append<float>, dim3(grid), dim3(64 * kAppendWaves), 0, s, g, p, layer,
-                           (const float *)k, (const float *)v, run_tok0, run_len);
+        rope_form(g) ? launch(float{}, std::true_type{}) : launch(float{}, std::false_type{});
     return hipGetLastError();
 }
 
@@ -1951,13 +1980,13 @@ int prefill_rows_per_pass() { return kPfRowsPerPass; }
 // tile per wave) or the full kPfRowsPerPass
 bool prefill_pass_rows_valid(int rows) { return rows == kPfRowsPerPass || rows == kPfWaves * 16; }
 
-template <int D, bool F8>
+template <int D, bool F8, bool RF>
 void launch_prefill_g(int G, dim3 grid, dim3 block, hipStream_t s, const PfArgs &pa) {
     switch (G) {
-        case 1: hipLaunchKernelGGL((k_prefill_mfma<D, 1, F8>), grid, block, 0, s, pa); break;
-        case 2: hipLaunchKernelGGL((k_prefill_mfma<D, 2, F8>), grid, block, 0, s, pa); break;
-        case 4: hipLaunchKernelGGL((k_prefill_mfma<D, 4, F8>), grid, block, 0, s, pa); break;
-        default: hipLaunchKernelGGL((k_prefill_mfma<D, 8, F8>), grid, block, 0, s, pa); break;
+        case 1: hipLaunchKernelGGL((k_prefill_mfma<D, 1, F8, RF>), grid, block, 0, s, pa); break;
+        case 2: hipLaunchKernelGGL((k_prefill_mfma<D, 2, F8, RF>), grid, block, 0, s, pa); break;
+        case 4: hipLaunchKernelGGL((k_prefill_mfma<D, 4, F8, RF>), grid, block, 0, s, pa); break;
+        default: hipLaunchKernelGGL((k_prefill_mfma<D, 8, F8, RF>), grid, block, 0, s, pa); break;
     }
 }
 
@@ -1975,12 +2004,19 @@ hipError_t launch_prefill_mfma(int dtype, const AttnArgs &a, const int32_t *item
     if (wgs > INT32_MAX) return hipErrorInvalidValue;
     PfArgs pa{a, items, zero_page, pass_rows};
     dim3 grid((unsigned)wgs), block(64 * kPfWaves);
-    if (dtype == 2)
-        launch_prefill_g<128, true>(G, grid, block, s, pa);
-    else if (a.g.d == 128)
-        launch_prefill_g<128, false>(G, grid, block, s, pa);
+    auto launch = [&](auto rf) {
+        constexpr bool RF = decltype(rf)::value;
+        if (dtype == 2)
+            launch_prefill_g<128, true, RF>(G, grid, block, s, pa);
+        else if (a.g.d == 128)
+            launch_prefill_g<128, false, RF>(G, grid, block, s, pa);
+        else
+            launch_prefill_g<64, false, RF>(G, grid, block, s, pa);
+    };
+    if (rope_form(a.g))
+        launch(std::true_type{});
     else
-        launch_prefill_g<64, false>(G, grid, block, s, pa);
+        launch(std::false_type{});
     return hipGetLastError();
 }
 

@@ -51,6 +51,7 @@ __device__ __forceinline__ f32x4_t mfma_pv(const uint2 &a, const uint2 &b, f32x4
 // fused RoPE + quantize + append: one wave per (token, kv head); lane i holds
 // the rotation pair (i, i + 64)
 // ---------------------------------------------------------------------------
+template <bool RF>
 __global__ __launch_bounds__(256) void k_append_fp8(PoolGeom g, PlanView p, int32_t layer,
                                                     const bf16_t *__restrict__ k,
                                                     const bf16_t *__restrict__ v) {
@@ -63,7 +64,7 @@ __global__ __launch_bounds__(256) void k_append_fp8(PoolGeom g, PlanView p, int3
     const bf16_t *kr = k + (row * g.hkv + h) * kF8D;
     const bf16_t *vr = v + (row * g.hkv + h) * kF8D;
     const float2 cs = p.rope[(int64_t)t * (kF8D / 2) + lane];
-    const float x0 = to_f32(kr[lane]), x1 = to_f32(kr[lane + 64]);
+    const float x0 = to_f32(kr[rope_a<RF>(g, lane)]), x1 = to_f32(kr[rope_b<RF>(g, lane, kF8D)]);
     const float y0 = fmaf(x0, cs.x, -x1 * cs.y);
     const float y1 = fmaf(x1, cs.x, x0 * cs.y);
     const float v0 = to_f32(vr[lane]), v1 = to_f32(vr[lane + 64]);
@@ -110,7 +111,7 @@ struct MfmaShape {
 #endif
 };
 
-template <int D, bool F8, int G, int NG, int NBUF>
+template <int D, bool F8, int G, int NG, int NBUF, bool RF>
 __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
     static_assert(D == kF8D || (D == 64 && !F8), "head dims with a block layout");
     constexpr int ND = D / 32;   // QK MFMAs per block
@@ -187,18 +188,26 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
     // ---- q prologue: rotate at pos, fold the softmax scale (log2 domain);
     // the B operand of QK MFMA s holds dims D/4 g4 + 8 s .. + 7 of head n.
     const int d0 = D / 4 * g4;
-    const int dp = d0 ^ (D / 2);  // RoPE partner dims
     uint4 qb[ND];
     const float2 *rp = a.p.rope + (int64_t)t * (D / 2) + (d0 & (D / 2 - 1));
     const float sgn = g4 < 2 ? -1.f : 1.f;
     {
         const bool hv = n < G;
         const bf16_t *qh = (const bf16_t *)a.q + (row * g.hq + (int64_t)kvh * G + (hv ? n : 0)) * D;
+        const bf16_t *qd = qh + d0, *qp = qh + (d0 ^ (D / 2));  // the dims and their partners
 #pragma unroll
         for (int s = 0; s < ND; ++s) {
             float x[8], y[8];
-            unpack8(((const uint4 *)(qh + d0))[s], x);
-            unpack8(((const uint4 *)(qh + dp))[s], y);
+            if constexpr (RF) {
+                const RopeSrc o = rope_src<RF>(g, d0 + 8 * s, 8, D);
+                uint4 xv = *(const uint4 *)(qh + o.x), yv = *(const uint4 *)(qh + o.y);
+                if (g.rope_il) rope_split(xv, yv, g4 >= 2);
+                unpack8(xv, x);
+                unpack8(yv, y);
+            } else {
+                unpack8(((const uint4 *)qd)[s], x);
+                unpack8(((const uint4 *)qp)[s], y);
+            }
             uint32_t w[4];
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
@@ -220,11 +229,19 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
         const bf16_t *vh = (const bf16_t *)a.v_new + (row * g.hkv + kvh) * D;
         if constexpr (VD == 1) {
             const float2 cs = rp[n];
-            const float k0 = fmaf(to_f32(kh[dd]), cs.x, sgn * to_f32(kh[dd ^ (D / 2)]) * cs.y);
+            int kd = dd, kp = dd ^ (D / 2);
+            if constexpr (RF) {
+                const int i0 = dd & (D / 2 - 1), ka = rope_a<RF>(g, i0), kb = rope_b<RF>(g, i0, D);
+                kd = g4 < 2 ? ka : kb;
+                kp = g4 < 2 ? kb : ka;
+            }
+            const float k0 = fmaf(to_f32(kh[kd]), cs.x, sgn * to_f32(kh[kp]) * cs.y);
             kc2 = from_f32<bf16_t>(k0).bits;  // rounded to the stored type as the append does
             vc2 = vh[dd].bits;
         } else {
-            const uint32_t kx = *(const uint32_t *)(kh + dd), ky = *(const uint32_t *)(kh + (dd ^ 64));
+            const RopeSrc o = rope_src<RF>(g, dd, 2, D);
+            uint32_t kx = *(const uint32_t *)(kh + o.x), ky = *(const uint32_t *)(kh + o.y);
+            if (RF && g.rope_il) rope_split(kx, ky, g4 >= 2);
             const uint32_t vx = *(const uint32_t *)(vh + dd);
             const float4 cs = *(const float4 *)(rp + 2 * n);  // (cos, sin) of dims dd, dd + 1
             const float k0 = fmaf(__uint_as_float(kx << 16), cs.x, sgn * __uint_as_float(ky << 16) * cs.y);
@@ -557,15 +574,18 @@ hipError_t launch_mfma_g(const AttnArgs &a, hipStream_t s) {
     const int64_t units = (int64_t)a.p.n_tok * a.g.hkv * a.n_split;
     if (units == 0) return hipSuccess;
     if (units > INT32_MAX) return hipErrorInvalidValue;  // one grid dimension, 32-bit unit index
-    hipLaunchKernelGGL((k_attn_mfma<D, F8, G, S::NG, S::NBUF>), dim3((unsigned)units), dim3(64 * S::NG),
-                       0, s, a);
+    const dim3 grid((unsigned)units), block(64 * S::NG);
+    if (rope_form(a.g))
+        hipLaunchKernelGGL((k_attn_mfma<D, F8, G, S::NG, S::NBUF, true>), grid, block, 0, s, a);
+    else
+        hipLaunchKernelGGL((k_attn_mfma<D, F8, G, S::NG, S::NBUF, false>), grid, block, 0, s, a);
     return hipGetLastError();
 }
 template <int D, bool F8, int G>
 int resident_mfma_g() {
     using S = MfmaShape<F8, G>;
     int n = 0;
-    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_attn_mfma<D, F8, G, S::NG, S::NBUF>,
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_attn_mfma<D, F8, G, S::NG, S::NBUF, false>,
                                                      64 * S::NG, 0) != hipSuccess)
         return 1;
     // The split rule fills these slots.  It counts the workgroups whose rings
@@ -635,8 +655,13 @@ hipError_t launch_append_fp8(const PoolGeom &g, const PlanView &p, int32_t layer
     if (g.d != kF8D) return hipErrorInvalidValue;
     const int64_t waves = (int64_t)p.n_tok * g.hkv;
     if (waves == 0) return hipSuccess;
-    hipLaunchKernelGGL(k_append_fp8, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, g, p, layer,
-                       (const bf16_t *)k, (const bf16_t *)v);
+    const dim3 grid((unsigned)((waves + 3) / 4)), block(256);
+    if (rope_form(g))
+        hipLaunchKernelGGL(k_append_fp8<true>, grid, block, 0, s, g, p, layer, (const bf16_t *)k,
+                           (const bf16_t *)v);
+    else
+        hipLaunchKernelGGL(k_append_fp8<false>, grid, block, 0, s, g, p, layer, (const bf16_t *)k,
+                           (const bf16_t *)v);
     return hipGetLastError();
 }
 

@@ -45,7 +45,7 @@ __device__ __forceinline__ f32x4_t mfma_f32(float a, float b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-template <int D, int G>
+template <int D, int G, bool RF>
 __global__ __launch_bounds__(64 * kF32Waves) void k_prefill_f32(F32Args pa) {
     constexpr int ROW = D * 4;            // bytes of a key row
     constexpr int TILE = kBlock * ROW;    // ... of a K (or V^T) tile
@@ -146,8 +146,10 @@ __global__ __launch_bounds__(64 * kF32Waves) void k_prefill_f32(F32Args pa) {
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int d0 = 16 * c + 4 * lg;
-            const float4 x = *(const float4 *)(qh + d0);
-            const float4 y = *(const float4 *)(qh + (d0 ^ (D / 2)));
+            const RopeSrc o = rope_src<RF>(g, d0, 4, D);
+            uint4 xb = *(const uint4 *)(qh + o.x), yb = *(const uint4 *)(qh + o.y);
+            if (RF && g.rope_il) rope_split_f32(xb, yb, d0 >= D / 2);
+            const float4 x = __builtin_bit_cast(float4, xb), y = __builtin_bit_cast(float4, yb);
             const float4 c0 = *(const float4 *)(rp + (d0 & (D / 2 - 1)));
             const float4 c1 = *(const float4 *)(rp + (d0 & (D / 2 - 1)) + 2);
             const float sg = d0 < D / 2 ? -1.f : 1.f;
@@ -365,14 +367,14 @@ __global__ __launch_bounds__(64 * kF32Waves) void k_prefill_f32(F32Args pa) {
     if (a.lse && lg == 0) a.lse[oh] = row_lse(m_ref, l);
 }
 
-template <int D>
+template <int D, bool RF>
 void launch_d(int G, dim3 grid, hipStream_t s, const F32Args &pa) {
     const dim3 block(64 * kF32Waves);
     switch (G) {
-        case 1: hipLaunchKernelGGL((k_prefill_f32<D, 1>), grid, block, 0, s, pa); break;
-        case 2: hipLaunchKernelGGL((k_prefill_f32<D, 2>), grid, block, 0, s, pa); break;
-        case 4: hipLaunchKernelGGL((k_prefill_f32<D, 4>), grid, block, 0, s, pa); break;
-        default: hipLaunchKernelGGL((k_prefill_f32<D, 8>), grid, block, 0, s, pa); break;
+        case 1: hipLaunchKernelGGL((k_prefill_f32<D, 1, RF>), grid, block, 0, s, pa); break;
+        case 2: hipLaunchKernelGGL((k_prefill_f32<D, 2, RF>), grid, block, 0, s, pa); break;
+        case 4: hipLaunchKernelGGL((k_prefill_f32<D, 4, RF>), grid, block, 0, s, pa); break;
+        default: hipLaunchKernelGGL((k_prefill_f32<D, 8, RF>), grid, block, 0, s, pa); break;
     }
 }
 
@@ -389,10 +391,11 @@ hipError_t launch_prefill_f32(const AttnArgs &a, const int32_t *items, int32_t n
     const int64_t wgs = (int64_t)n_items * a.g.hkv * a.n_split;
     if (wgs > INT32_MAX) return hipErrorInvalidValue;
     const F32Args pa{a, items};
-    if (a.g.d == 128)
-        launch_d<128>(G, dim3((unsigned)wgs), s, pa);
+    const dim3 grid((unsigned)wgs);
+    if (rope_form(a.g))
+        a.g.d == 128 ? launch_d<128, true>(G, grid, s, pa) : launch_d<64, true>(G, grid, s, pa);
     else
-        launch_d<64>(G, dim3((unsigned)wgs), s, pa);
+        a.g.d == 128 ? launch_d<128, false>(G, grid, s, pa) : launch_d<64, false>(G, grid, s, pa);
     return hipGetLastError();
 }
 
