@@ -204,6 +204,35 @@ mtn_status mtn_session_open(mtn_pool *pool, int32_t *sid_out);
 mtn_status mtn_session_close(mtn_pool *pool, int32_t sid);
 
 /*
+ * Fork a session into n_copies new ones (lowest free ids, in sids_out, host):
+ * every page it holds, of every layer, is copied on `stream`, so source and
+ * copies go on independently, as sessions that were fed the same tokens.  A page is
+ * read once for up to 32 copies.  The copies' blocks are the lowest free ones,
+ * copy after copy, in order of logical block.  Windowed pools reserve each
+ * copy's whole footprint as mtn_session_open does.  Errors:
+ * MTN_ERR_BAD_SESSION, MTN_ERR_NO_SESSION_SLOT, MTN_ERR_POOL_EXHAUSTED,
+ * MTN_ERR_BAD_STATE while a plan is open or the stream is being captured,
+ * MTN_ERR_DEVICE.  The next plan may use another stream, as after a plan.
+ */
+mtn_status mtn_session_fork(mtn_pool *pool, int32_t sid, int32_t n_copies, int32_t *sids_out /*host*/,
+                            void *stream);
+
+/*
+ * Move the pool into another buffer with n_blocks blocks, larger or smaller:
+ * kv_dev (device, caller-owned, 256-byte aligned, >= mtn_pool_required_bytes for
+ * the pool's config with n_blocks, not overlapping the present one).  Every
+ * page is copied on `stream`; the pages take blocks 0, 1, ... of the new buffer in
+ * order of session id and logical block, the rest of it is left as it is and
+ * free.  Lengths, session ids and results do not change.  The old buffer is the
+ * caller's again once the work issued on `stream` so far is done.
+ * MTN_ERR_POOL_EXHAUSTED if the sessions hold or (windowed) have reserved more
+ * than n_blocks, MTN_ERR_BAD_STATE while a plan is open or the stream is being
+ * captured.  Host-only pools: kv_dev may be NULL.
+ */
+mtn_status mtn_pool_resize(mtn_pool *pool, int64_t n_blocks, void *kv_dev, size_t kv_bytes,
+                           void *stream);
+
+/*
  * Plans.  Positions advance once per token, not per layer, so per-layer calls
  * act on one open plan:
  *

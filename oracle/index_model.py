@@ -139,6 +139,53 @@ class IndexModel:
             self.reserved -= self.row_len
         del self.sessions[sid]
 
+    def fork(self, sid: int, copies: int) -> List[int]:
+        """Copies of a session: fresh blocks, lowest first, copy after copy."""
+        if self.plan is not None:
+            raise IndexError_(ERR_BAD_STATE, "plan open")
+        if copies < 1:
+            raise IndexError_(ERR_INVALID_ARG, "copies < 1")
+        if sid not in self.sessions:
+            raise IndexError_(ERR_BAD_SESSION, "not open")
+        ids = [i for i in range(self.max_sessions) if i not in self.sessions][:copies]
+        if len(ids) < copies:
+            raise IndexError_(ERR_NO_SESSION_SLOT, "no free session slot")
+        s = self.sessions[sid]
+        held = [lb for lb, b in enumerate(s.row) if b >= 0]
+        if self.window is not None:
+            if self.reserved + copies * self.row_len > self.n_blocks:
+                raise IndexError_(ERR_POOL_EXHAUSTED, "reservation exceeds pool")
+            self.reserved += copies * self.row_len
+        elif copies * len(held) > len(self.free):
+            raise IndexError_(ERR_POOL_EXHAUSTED, "pool exhausted")
+        for i in ids:
+            row = [-1] * self.row_len
+            for lb in held:
+                row[lb] = heapq.heappop(self.free)
+            self.sessions[i] = _Session(s.length, row)
+        return ids
+
+    def resize(self, n_blocks: int) -> Dict[int, int]:
+        """Another number of blocks; pages renumbered from 0 in order of session
+        and logical block.  Returns {old block: new block}."""
+        if self.plan is not None:
+            raise IndexError_(ERR_BAD_STATE, "plan open")
+        if n_blocks < 1:
+            raise IndexError_(ERR_INVALID_ARG, "n_blocks < 1")
+        if max(self.assigned(), self.reserved_blocks()) > n_blocks:
+            raise IndexError_(ERR_POOL_EXHAUSTED, "sessions hold more")
+        moved: Dict[int, int] = {}
+        for sid in sorted(self.sessions):
+            row = self.sessions[sid].row
+            for lb, b in enumerate(row):
+                if b >= 0:
+                    moved[b] = len(moved)
+                    row[lb] = moved[b]
+        self.n_blocks = n_blocks
+        self.free = list(range(len(moved), n_blocks))
+        heapq.heapify(self.free)
+        return moved
+
     # -- planning ----------------------------------------------------------
     def plan_begin(self, sids: Sequence[int], n_tok: Sequence[int]) -> None:
         if self.plan is not None:

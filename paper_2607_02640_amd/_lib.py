@@ -44,7 +44,7 @@ EXPORTS = [
     "mtn_pool_required_bytes", "mtn_pool_create", "mtn_pool_destroy",
     "mtn_session_open", "mtn_session_close", "mtn_plan_begin", "mtn_plan_commit",
     "mtn_plan_abort",
-    "mtn_pool_set_rope",
+    "mtn_pool_set_rope", "mtn_session_fork", "mtn_pool_resize",
     "mtn_frame_append_kv", "mtn_attend_chunk_prefill", "mtn_attend_decode",
     "mtn_attend_decode_append", "mtn_attend_decode_noalloc",
     "mtn_frame_step", "mtn_pool_stats", "mtn_session_info", "mtn_session_block_table",
@@ -132,6 +132,8 @@ def load() -> C.CDLL:
         "mtn_pool_create": (i32, [C.POINTER(PoolConfig), vp, C.c_size_t, vp, C.POINTER(vp)]),
         "mtn_pool_destroy": (None, [vp]),
         "mtn_pool_set_rope": (i32, [vp, C.POINTER(RopeConfig)]),
+        "mtn_session_fork": (i32, [vp, i32, i32, P32, vp]),
+        "mtn_pool_resize": (i32, [vp, i64, vp, C.c_size_t, vp]),
         "mtn_session_open": (i32, [vp, P32]),
         "mtn_session_close": (i32, [vp, i32]),
         "mtn_plan_begin": (i32, [vp, i32, P32, P32, vp]),
@@ -276,6 +278,28 @@ class Pool:
 
     def session_close(self, sid: int) -> None:
         self._check(self.lib.mtn_session_close(self.h, sid), "session_close")
+
+    def session_fork(self, sid: int, copies: int = 1, stream=None) -> list:
+        """New sessions that hold what session ``sid`` holds; their ids."""
+        out = (C.c_int32 * max(copies, 1))()
+        self._check(self.lib.mtn_session_fork(self.h, sid, copies, out,
+                                              None if self.host_only else _stream(stream)), "session_fork")
+        return list(out[:copies])
+
+    def resize(self, n_blocks: int, kv=None, stream=None) -> None:
+        """Move every page into the buffer ``kv`` with ``n_blocks`` blocks; the
+        pool then holds ``kv`` and no longer the buffer before it."""
+        size = C.c_size_t(kv.numel() * kv.element_size() if kv is not None else 0)
+        if self.kv is not None:  # torch may not hand the old buffer out before the copy has run
+            import torch
+            self.kv.record_stream(torch.cuda.current_stream() if stream is None
+                                  else torch.cuda.ExternalStream(stream))
+        self._check(self.lib.mtn_pool_resize(self.h, n_blocks, _ptr(kv), size,
+                                             None if self.host_only else _stream(stream)), "resize")
+        self.cfg.n_blocks = n_blocks
+        n = C.c_size_t()
+        self._check(self.lib.mtn_pool_required_bytes(C.byref(self.cfg), C.byref(n)), "resize")
+        self.required_bytes, self.kv = n.value, kv
 
     def plan_begin(self, sids, n_tok, stream=None) -> None:
         st = self.lib.mtn_plan_begin(self.h, len(sids), _arr32(sids), _arr32(n_tok),

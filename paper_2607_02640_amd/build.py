@@ -24,7 +24,7 @@ COMMON = [
 ]
 
 SOURCES = ["mtn_host.cpp", "mtn_admission.cpp", "mtn_kernels.hip", "mtn_mfma.hip",
-           "mtn_prefill_f32.hip"]
+           "mtn_prefill_f32.hip", "mtn_pages.hip"]
 
 # Per-source code generation.  The matrix-core decode takes its MFMA
 # accumulators in ordinary VGPRs: in the AGPR form the compiler copied the 32

@@ -503,6 +503,67 @@ void plan_prefill(mtn_pool *P) {
         });
 }
 
+// Make `stream` follow everything issued on the previous plan's (or page
+// operation's) stream; later ones follow `stream`.
+mtn_status follow_last_stream(mtn_pool *P, void *stream) {
+    if (P->host_only) return MTN_OK;
+    if (P->have_last_stream && stream != P->last_stream) {
+        HIP_TRY(P, hipEventRecord(P->order_ev, (hipStream_t)P->last_stream));
+        HIP_TRY(P, hipStreamWaitEvent((hipStream_t)stream, P->order_ev, 0));
+    }
+    P->have_last_stream = true;
+    P->last_stream = stream;
+    return MTN_OK;
+}
+
+// Page operations change the host's tables as they are called, so a captured
+// one could not be replayed.
+mtn_status refuse_capture(mtn_pool *P, void *stream) {
+    if (P->host_only) return MTN_OK;
+    hipStreamCaptureStatus c = hipStreamCaptureStatusNone;
+    const hipError_t e = hipStreamIsCapturing((hipStream_t)stream, &c);
+    if (e == hipSuccess && c == hipStreamCaptureStatusNone) return MTN_OK;
+    (void)hipGetLastError();
+    return fail(P, MTN_ERR_BAD_STATE, "page operations cannot be captured");
+}
+
+// Sink blocks among a session's assigned ones.  Slots fill from the first on,
+// the sinks' before the ring's: the assigned logical blocks are 0 .. n - 1 of
+// the sinks and 0 .. n_assigned - n - 1 of the ring.
+int32_t sink_pages(const mtn_pool *P, int32_t sid) { return std::min(P->n_assigned[sid], P->nsb); }
+int32_t page_lb(const mtn_pool *P, int32_t sid, int32_t i) {
+    const int32_t n = sink_pages(P, sid);
+    return i < n ? i : P->nsb + (i - n);
+}
+
+// The fork's device work: the source's pages into the blocks that the copies'
+// table rows name, and those rows.
+mtn_status fork_pages(mtn_pool *P, int32_t src, const std::vector<int32_t> &sids, hipStream_t s) {
+    const int32_t pages = P->n_assigned[src];
+    ForkArgs a;
+    a.kv = P->kv;
+    a.layer_stride = P->layer_stride;
+    a.block_stride = P->block_stride;
+    a.table = P->d_table;
+    a.row_len = P->row_len;
+    a.n_sink_blocks = P->nsb;
+    a.src = src;
+    a.n_sink_pages = sink_pages(P, src);
+    for (size_t c0 = 0; c0 < sids.size(); c0 += kForkCopies) {
+        a.copies = (int32_t)std::min<size_t>(kForkCopies, sids.size() - c0);
+        for (int32_t c = 0; c < a.copies; ++c) a.sid[c] = sids[c0 + c];
+        for (a.first = 0; a.first < pages; a.first += a.m) {
+            a.m = std::min(kForkBlocks / a.copies, pages - a.first);
+            for (int32_t c = 0; c < a.copies; ++c)
+                for (int32_t i = 0; i < a.m; ++i)
+                    a.block[c * a.m + i] =
+                        P->table[(size_t)a.sid[c] * P->row_len + page_lb(P, src, a.first + i)];
+            HIP_TRY(P, launch_fork(a, P->cfg.n_layers, s));
+        }
+    }
+    return MTN_OK;
+}
+
 // Internal plan begin.  rows == nullptr packs io rows in plan order.
 mtn_status plan_begin(mtn_pool *P, int32_t n_seq, const int32_t *sids, const int32_t *n_tok,
                       const int32_t *rows, void *stream) {
@@ -537,14 +598,7 @@ mtn_status plan_begin(mtn_pool *P, int32_t n_seq, const int32_t *sids, const int
             need += new_blocks_needed(P, sids[i], P->len[sids[i]], n_tok[i], lbseen);
         if (need > P->alloc.n_free()) return fail(P, MTN_ERR_POOL_EXHAUSTED, "pool exhausted");
     }
-    if (!P->host_only) {
-        if (P->have_last_stream && stream != P->last_stream) {
-            HIP_TRY(P, hipEventRecord(P->order_ev, (hipStream_t)P->last_stream));
-            HIP_TRY(P, hipStreamWaitEvent((hipStream_t)stream, P->order_ev, 0));
-        }
-        P->have_last_stream = true;
-        P->last_stream = stream;
-    }
+    if (mtn_status st = follow_last_stream(P, stream)) return st;
     // ---- assignment (lowest free first, plan order)
     P->n_seq = n_seq;
     P->T = (int32_t)T;
@@ -1357,6 +1411,134 @@ mtn_status mtn_session_close(mtn_pool *P, int32_t sid) {
         // The device copy of the row is left as is: kernels still in flight may
         // read it, and a reopened session only ever reads logical blocks that its
         // own plans assigned (and uploaded, in stream order) again.
+        return MTN_OK;
+    });
+}
+
+mtn_status mtn_session_fork(mtn_pool *P, int32_t sid, int32_t n_copies, int32_t *sids_out,
+                            void *stream) {
+    return guarded(P, [&]() -> mtn_status {
+        if (!P) return MTN_ERR_INVALID_ARG;
+        if (P->plan_open) return fail(P, MTN_ERR_BAD_STATE, "plan open");
+        if (mtn_status st = refuse_capture(P, stream)) return st;
+        if (n_copies < 1 || !sids_out) return fail(P, MTN_ERR_INVALID_ARG, "n_copies < 1 or null array");
+        if (sid < 0 || sid >= P->cfg.max_sessions || !P->is_open[sid])
+            return fail(P, MTN_ERR_BAD_SESSION, "session not open");
+        if (n_copies > P->cfg.max_sessions - P->n_open)
+            return fail(P, MTN_ERR_NO_SESSION_SLOT, "no free session slot");
+        const int64_t pages = P->n_assigned[sid];
+        if (P->unbounded ? pages * n_copies > P->alloc.n_free()
+                         : P->reserved + (int64_t)n_copies * P->row_len > P->cfg.n_blocks)
+            return fail(P, MTN_ERR_POOL_EXHAUSTED, "no room for the copies");
+        std::vector<int32_t> sids;
+        sids.reserve((size_t)n_copies);
+        for (int32_t i = 0; (int32_t)sids.size() < n_copies; ++i)
+            if (!P->is_open[i]) sids.push_back(i);
+        mtn_status st = launch_gate(P);
+        if (!st) st = follow_last_stream(P, stream);
+        if (st) return st;
+        for (const int32_t c : sids) {
+            int32_t *row = &P->table[(size_t)c * P->row_len];
+            for (int32_t i = 0; i < pages; ++i) row[page_lb(P, sid, i)] = (int32_t)P->alloc.take();
+        }
+        if (!P->host_only && pages) {
+            st = fork_pages(P, sid, sids, (hipStream_t)stream);
+            if (st) {  // the blocks go back; what a launch wrote lies in free blocks
+                for (const int32_t c : sids) {
+                    int32_t *row = &P->table[(size_t)c * P->row_len];
+                    for (int32_t i = 0; i < pages; ++i) {
+                        int32_t &b = row[page_lb(P, sid, i)];
+                        P->alloc.give(b);
+                        b = -1;
+                    }
+                }
+                return st;
+            }
+        }
+        for (const int32_t c : sids) {
+            P->is_open[c] = 1;
+            P->len[c] = P->len[sid];
+            P->n_assigned[c] = (int32_t)pages;
+        }
+        P->n_open += n_copies;
+        P->assigned += pages * n_copies;
+        P->reserved = P->unbounded ? P->assigned : P->reserved + (int64_t)n_copies * P->row_len;
+        std::copy(sids.begin(), sids.end(), sids_out);
+        return MTN_OK;
+    });
+}
+
+mtn_status mtn_pool_resize(mtn_pool *P, int64_t n_blocks, void *kv_dev, size_t kv_bytes, void *stream) {
+    return guarded(P, [&]() -> mtn_status {
+        if (!P) return MTN_ERR_INVALID_ARG;
+        if (P->plan_open) return fail(P, MTN_ERR_BAD_STATE, "plan open");
+        if (mtn_status st = refuse_capture(P, stream)) return st;
+        if (n_blocks < 1 || n_blocks > INT32_MAX) return fail(P, MTN_ERR_INVALID_ARG, "bad n_blocks");
+        mtn_pool_config cfg = P->cfg;
+        cfg.n_blocks = n_blocks;
+        size_t need = 0, have = 0;
+        mtn_status st = mtn_pool_required_bytes(&cfg, &need);
+        if (!st) st = mtn_pool_required_bytes(&P->cfg, &have);
+        if (st) return fail(P, st, "bad size");
+        if (!P->host_only) {
+            const uintptr_t a = (uintptr_t)P->kv, b = (uintptr_t)kv_dev;
+            if (!kv_dev || (b & 255) || kv_bytes < need)
+                return fail(P, MTN_ERR_INVALID_ARG, "null, misaligned or small buffer");
+            if (b < a + have && a < b + need) return fail(P, MTN_ERR_INVALID_ARG, "the buffers overlap");
+        }
+        if (std::max(P->assigned, P->reserved) > n_blocks)
+            return fail(P, MTN_ERR_POOL_EXHAUSTED, "sessions hold more blocks");
+        // pages take blocks 0, 1, ... in order of session and logical block
+        std::vector<MoveSession> moves;
+        moves.reserve((size_t)P->n_open);
+        int32_t base = 0;
+        for (int32_t sid = 0; sid < P->cfg.max_sessions; ++sid) {
+            if (!P->is_open[sid] || !P->n_assigned[sid]) continue;
+            moves.push_back({sid, base, P->n_assigned[sid], sink_pages(P, sid)});
+            base += P->n_assigned[sid];
+        }
+        BlockAllocator alloc;
+        alloc.reset(n_blocks);
+        for (int32_t b = 0; b < base; ++b) alloc.take();
+        st = launch_gate(P);
+        if (!st) st = follow_last_stream(P, stream);
+        if (st) return st;
+        const int64_t layer_stride = P->block_stride * n_blocks;
+        if (!P->host_only && !moves.empty()) {
+            MoveArgs a;
+            a.kv = P->kv;
+            a.to = (uint8_t *)kv_dev;
+            a.layer_stride = P->layer_stride;
+            a.to_layer_stride = layer_stride;
+            a.block_stride = P->block_stride;
+            a.table = P->d_table;
+            a.row_len = P->row_len;
+            a.n_sink_blocks = P->nsb;
+            auto each = [&](auto &&launch) {
+                hipError_t e = hipSuccess;
+                for (size_t i = 0; i < moves.size() && e == hipSuccess; i += kMoveSessions) {
+                    a.n = (int32_t)std::min<size_t>(kMoveSessions, moves.size() - i);
+                    std::copy_n(&moves[i], a.n, a.s);
+                    e = launch();
+                }
+                return e;
+            };
+            HIP_TRY(P, each([&] { return launch_move(a, P->cfg.n_layers, (hipStream_t)stream); }));
+            const hipError_t e = each([&] { return launch_move_table(a, (hipStream_t)stream); });
+            if (e != hipSuccess) {  // back to the tables of the old buffer
+                (void)hipStreamSynchronize((hipStream_t)stream);
+                (void)hipMemcpy(P->d_table, P->table.data(), sizeof(int32_t) * P->table.size(),
+                                hipMemcpyHostToDevice);
+                return hip_fail(P, e, "launch_move_table");
+            }
+        }
+        for (const MoveSession &m : moves)
+            for (int32_t i = 0; i < m.pages; ++i)
+                P->table[(size_t)m.sid * P->row_len + page_lb(P, m.sid, i)] = m.base + i;
+        P->alloc = std::move(alloc);
+        P->cfg.n_blocks = n_blocks;
+        P->layer_stride = layer_stride;
+        P->kv = (uint8_t *)kv_dev;
         return MTN_OK;
     });
 }

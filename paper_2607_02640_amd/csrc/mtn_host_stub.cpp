@@ -36,6 +36,9 @@ hipError_t launch_copy(const void *, void *, size_t, hipStream_t) { return hipEr
 hipError_t launch_read(const void *, size_t, uint32_t *, hipStream_t) {
     return hipErrorNotSupported;
 }
+hipError_t launch_fork(const ForkArgs &, int32_t, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_move(const MoveArgs &, int32_t, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_move_table(const MoveArgs &, hipStream_t) { return hipErrorNotSupported; }
 hipError_t scratch_buffer(float **, size_t *) { return hipErrorNotSupported; }
 int fp8_head_stride(int d) { return d == 128 ? 4224 : 0; }
 static bool group_ok(int g) { return g == 1 || g == 2 || g == 4 || g == 8; }

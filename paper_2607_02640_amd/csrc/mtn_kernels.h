@@ -112,6 +112,39 @@ hipError_t launch_copy(const void *src, void *dst, size_t bytes, hipStream_t s);
 // computed or written)
 hipError_t launch_read(const void *src, size_t bytes, uint32_t *out, hipStream_t s);
 
+// Fork: pages first .. first + m - 1 of session src into `copies` new sessions;
+// copy c of page first + i is block[c * m + i].  n_sink_pages: how many of the
+// session's pages are sink blocks (the rest are its ring's, from the first on).
+constexpr int kForkCopies = 32, kForkBlocks = 896;  // per launch (kernel arguments hold at most 4 KiB)
+struct ForkArgs {
+    uint8_t *kv;
+    int64_t layer_stride, block_stride;
+    int32_t *table;
+    int32_t row_len, n_sink_blocks;
+    int32_t src, n_sink_pages, first, m, copies;
+    int32_t sid[kForkCopies];
+    int32_t block[kForkBlocks];
+};
+hipError_t launch_fork(const ForkArgs &a, int32_t n_layers, hipStream_t s);
+
+// Move: page i of session s[k] becomes block s[k].base + i of the buffer `to`;
+// launch_move copies, launch_move_table then rewrites the block tables.
+constexpr int kMoveSessions = 240;
+struct MoveSession {
+    int32_t sid, base, pages, n_sink_pages;
+};
+struct MoveArgs {
+    const uint8_t *kv;
+    uint8_t *to;
+    int64_t layer_stride, to_layer_stride, block_stride;
+    int32_t *table;
+    int32_t row_len, n_sink_blocks;
+    int32_t n;
+    MoveSession s[kMoveSessions];
+};
+hipError_t launch_move(const MoveArgs &a, int32_t n_layers, hipStream_t s);
+hipError_t launch_move_table(const MoveArgs &a, hipStream_t s);
+
 // The library's static device workspace for split partials (a file-scope
 // array, no allocation): its address on the current device and its size in
 // floats.
