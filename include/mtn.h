@@ -45,7 +45,17 @@
  *     to [-126, 127], 0 for an all-zero row); its q/k/v/out are bf16
  *     (io_dtype MTN_BF16) and it needs head_dim 128.  Per-token KV
  *     reduction composes with the window bound (Metronome §4.1, closing
- *     remark; §6).  Accumulation is fp32; bf16 results are rounded to
+ *     remark; §6).  kv_dtype MTN_INT8_BLOCK (bf16 io, head_dim 64 or 128)
+ *     stores int8 codes under one fp32 scale per block of 16 tokens, KV head
+ *     and tensor.  A block (sinks 16b .. min(S, 16b + 16) - 1, or S + 16j .. + 15)
+ *     is quantized when the last of its positions is appended: with s =
+ *     max|x| / 127 over its rows (1 where all are zero) code = x / s rounded to
+ *     the nearest integer, ties to even, and the block's keys read as code * s
+ *     from that append on (NaN throughout a block, head and tensor with a
+ *     non-finite element).  Rows of a block that is still open read as they
+ *     were appended (keys rotated, then rounded to bf16).  Every row is
+ *     rounded to 8 bits once, and the same whatever plans brought it.
+ *     Accumulation is fp32; bf16 results are rounded to
  *     nearest-even.
  */
 #ifndef MTN_H
@@ -75,7 +85,7 @@ typedef int32_t mtn_status;
 #define MTN_ERR_HOST_MEMORY     (-10) /* a host allocation failed (no C++
                                          exception ever leaves the library)    */
 
-enum { MTN_F32 = 0, MTN_BF16 = 1, MTN_FP8_E4M3 = 2 };
+enum { MTN_F32 = 0, MTN_BF16 = 1, MTN_FP8_E4M3 = 2, MTN_INT8_BLOCK = 3 };
 
 /* window value selecting the unbounded (vanilla) policy: no window, no
  * eviction, sinks ignored, linear block table up to max_len tokens.          */
@@ -102,8 +112,8 @@ typedef struct {
     int32_t  max_sessions;  /* >= 1 concurrently open sessions                 */
     int32_t  max_len;       /* unbounded only: per-session token cap (>= 1)    */
     int64_t  n_blocks;      /* pool capacity in blocks (>= 1)                  */
-    int32_t  kv_dtype;      /* MTN_F32 | MTN_BF16 | MTN_FP8_E4M3               */
-    int32_t  io_dtype;      /* kv_dtype, or MTN_BF16 for an MTN_FP8_E4M3 cache */
+    int32_t  kv_dtype;      /* MTN_F32 | MTN_BF16 | MTN_FP8_E4M3 | MTN_INT8_BLOCK */
+    int32_t  io_dtype;      /* kv_dtype, or MTN_BF16 for an 8-bit cache        */
     double   rope_theta;    /* RoPE base (> 1)                                 */
     float    softmax_scale; /* 0 selects 1/sqrt(head_dim)                      */
     uint32_t flags;         /* MTN_POOL_* flags                                */
@@ -128,6 +138,15 @@ typedef struct {
  *   K exponents e + 127, one byte per key    bytes [4096, 4112)
  *   V exponents e + 127                      bytes [4112, 4128)
  * and 96 bytes of padding; a stored value is code * 2^e.
+ *
+ * MTN_INT8_BLOCK: each (l, b) region is Hkv * (32 D + 8) bytes, padded to 128, at
+ * (l * n_blocks + b) times that, and holds per head h
+ *   K codes + 128, unsigned [16][D]          bytes [h * 32 D, + 16 D)
+ *   V codes, signed, in key quads: byte ((key / 4) * D + d) * 4 + key % 4 after them
+ *   the scales {K, V}, fp32                  bytes [Hkv * 32 D + 8 h, + 8)
+ * Behind the blocks (256-byte aligned) lie two tails per session slot, [layer]
+ * [Hkv]{K [16][D], V [16][D]} bf16: the rows of the session's open block (two, so
+ * that an abandoned plan leaves the committed rows whole).
  */
 mtn_status mtn_pool_required_bytes(const mtn_pool_config *cfg, size_t *kv_bytes);
 
@@ -293,7 +312,7 @@ mtn_status mtn_frame_append_kv(mtn_pool *pool, int32_t layer, const void *k, con
  * position t is rotated at t and attends to sinks [0, min(S, t+1)) and window
  * [max(S, t-W+1), t] of its own session (all earlier chunk tokens included).
  * lse: device [T][Hq] fp32 natural-log sum-exp of the scaled scores, or NULL.
- * bf16 and fp8 pools run the bf16 MFMA kernel, fp32 pools an fp32 MFMA kernel.
+ * bf16 and 8-bit pools run the bf16 MFMA kernel, fp32 pools an fp32 MFMA kernel.
  */
 mtn_status mtn_attend_chunk_prefill(mtn_pool *pool, int32_t layer, const void *q, void *out,
                                     float *lse, void *stream);
@@ -410,7 +429,9 @@ mtn_status mtn_plan_info(const mtn_pool *pool, int64_t *pos, int32_t *block, int
 
 /* Debug: write NaN into every slot that no query may read: all unassigned
  * blocks, sink-block slots at or past S, and ring slots of positions outside
- * each open session's retained set.  Attention results must not change.       */
+ * each open session's retained set (int8 pools: codes of +127 there, NaN scales in
+ * blocks without a live slot, NaN in unused rows of the tails).  Attention
+ * results must not change.                                                    */
 mtn_status mtn_debug_poison_dead(mtn_pool *pool, void *stream);
 
 /* Tuning: query rows per chunk-prefill pass (rows are token x G + group head;
@@ -425,7 +446,7 @@ mtn_status mtn_pool_set_prefill_pass_rows(mtn_pool *pool, int32_t rows);
 
 /* Test / tuning: the decode kernel.  0 (default) chooses by shape; 1 forces
  * the vector kernel (fp32 and bf16 pools); 2 forces the matrix-core kernel
- * (bf16 pools with head_dim 128; FP8 pools always use it; at head_dim 64 the
+ * (bf16 pools with head_dim 128; 8-bit pools always use theirs; at head_dim 64 the
  * automatic choice alone takes it).  Takes effect at the next launch; results
  * agree up to fp32 summation order.  MTN_ERR_UNSUPPORTED where the kernel
  * does not exist for the pool or cannot be forced, MTN_ERR_BAD_STATE while a

@@ -28,6 +28,9 @@ Modules
     the FP8 KV cache (per-token KV reduction composes with the window, §4.1
     and §6), written from the format's definition; ``OracleSession`` applies
     it to every stored row when ``kv_quant="fp8_e4m3"``.
+``int8_kv``
+    The int8 KV block: one scale per block of 16 tokens and head, applied when a
+    block is complete (``kv_quant="int8_block"``).
 
 Parity status of each function is stated in its module header.
 """

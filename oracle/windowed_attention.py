@@ -36,7 +36,8 @@ Nothing is rounded: inputs are widened to float64 exactly (bf16 and fp32 are
 both exactly representable) and every step runs in float64.  The one
 exception is opt-in: ``kv_quant="fp8_e4m3"`` stores every K/V row through the
 E4M3 codec of ``fp8_kv`` (per-token KV reduction, §4.1 / §6), and attention
-reads the exact dequantized values.
+reads the exact dequantized values; ``kv_quant="int8_block"`` does so with
+the complete blocks of ``int8_kv``, keys rounded to bf16 before.
 """
 from __future__ import annotations
 
@@ -45,6 +46,7 @@ from typing import Dict, List, Optional, Sequence, Tuple
 
 import numpy as np
 
+from . import int8_kv
 from .fp8_kv import roundtrip_row
 
 UNBOUNDED = None  # window value that means "no window" (the vanilla policy)
@@ -218,9 +220,12 @@ class OracleSession:
         self.n_layers = n_layers
         self.literal = literal_window
         self.check_psum = check_psum
-        if kv_quant not in (None, "fp8_e4m3"):
-            raise ValueError("kv_quant must be None or 'fp8_e4m3'")
+        if kv_quant not in (None, "fp8_e4m3", "int8_block"):
+            raise ValueError("kv_quant must be None, 'fp8_e4m3' or 'int8_block'")
         self.kv_quant = kv_quant
+        # int8: every layer's rows of the open block, by position (kept whole
+        # until the block is complete, also where the window has passed them)
+        self.open_rows: List[Dict[int, Tuple[np.ndarray, np.ndarray]]] = [{} for _ in range(n_layers)]
         self.length = 0
         self.state: List[Dict[int, Tuple[np.ndarray, np.ndarray]]] = [
             {} for _ in range(n_layers)]
@@ -269,7 +274,12 @@ class OracleSession:
                 # through the E4M3 codec with its own power-of-two scale
                 kr = np.stack([roundtrip_row(kr[h], True) for h in range(self.hkv)])
                 vi = np.stack([roundtrip_row(vi[h], True) for h in range(self.hkv)])
+            if self.kv_quant == "int8_block":
+                kr = int8_kv.bf16(kr)
+                self.open_rows[layer][base + i] = (kr, vi)
             st[base + i] = (kr, vi)
+        if self.kv_quant == "int8_block":
+            self._close_blocks(layer, base + c)
         self._done.add(layer)
         if not attend:
             return None
@@ -292,6 +302,22 @@ class OracleSession:
                 out[i, h] = o
                 lse[i, h] = l
         return out, lse
+
+    def _close_blocks(self, layer: int, end: int) -> None:
+        """Quantize the blocks that end at or before position ``end``."""
+        rows = self.open_rows[layer]
+        while rows:
+            lo, hi = int8_kv.block_span(min(rows), self.n_sink)
+            if hi > end:
+                return
+            held = [rows.pop(p) for p in range(lo, hi)]
+            for x in range(2):  # keys, values
+                r = np.stack([h[x] for h in held])  # [n, Hkv, D]
+                q = np.stack([int8_kv.roundtrip_block(r[:, h]) for h in range(self.hkv)], axis=1)
+                for p in range(lo, hi):
+                    kv = self.state[layer].get(p)
+                    if kv is not None:
+                        self.state[layer][p] = (q[p - lo], kv[1]) if x == 0 else (kv[0], q[p - lo])
 
     def commit(self) -> Tuple[int, int]:
         c = self._pending

@@ -30,9 +30,11 @@ MTN_ERR_HOST_MEMORY = -10
 MTN_F32 = 0
 MTN_BF16 = 1
 MTN_FP8_E4M3 = 2
-# pool dtype name -> (kv_dtype, io_dtype); "fp8" keeps E4M3 codes with bf16 io
+MTN_INT8_BLOCK = 3
+# pool dtype name -> (kv_dtype, io_dtype); "fp8" keeps E4M3 codes, "int8" int8
+# codes under one scale per block and head, both with bf16 io
 DTYPES = {"f32": (MTN_F32, MTN_F32), "bf16": (MTN_BF16, MTN_BF16),
-          "fp8": (MTN_FP8_E4M3, MTN_BF16)}
+          "fp8": (MTN_FP8_E4M3, MTN_BF16), "int8": (MTN_INT8_BLOCK, MTN_BF16)}
 MTN_WINDOW_UNBOUNDED = -1
 MTN_POOL_HOST_ONLY = 1
 # rotary forms of Pool.set_rope

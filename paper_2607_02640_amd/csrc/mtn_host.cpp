@@ -87,6 +87,7 @@ struct mtn_pool {
     mtn_pool_config cfg;
     bool host_only = false;
     bool unbounded = false;
+    bool int8 = false;         // int8 codes under block scales, open blocks in tails
     int S = 0, W = -1, R = 0, nsb = 0, row_len = 0, G = 1;
     size_t elt = 4;
     int64_t tile_bytes = 0, head_stride = 0, block_stride = 0, layer_stride = 0;
@@ -98,6 +99,10 @@ struct mtn_pool {
     std::vector<uint8_t> is_open;
     std::vector<int64_t> len;
     std::vector<int32_t> n_assigned;
+    // int8 pools: which of a session's two tails holds the rows of its open block.
+    // A plan that begins a block uses the other one, so that the committed rows
+    // stay whole until the plan commits.
+    std::vector<uint8_t> tail;
     BlockAllocator alloc;
     int64_t assigned = 0, reserved = 0;
     int32_t n_open = 0;
@@ -110,6 +115,7 @@ struct mtn_pool {
     bool pf_one_pass = false;  // every sequence takes one chunk-prefill row pass
     std::vector<int32_t> seq_sid, seq_ntok, seq_first;
     std::vector<int64_t> seq_pos0;
+    std::vector<uint8_t> seq_tail;  // int8 pools: the tail of each sequence's last block
     std::vector<int32_t> tok_sid, tok_pos, tok_row, tok_block, tok_off;
     std::vector<int32_t> upd_idx, upd_val;
     std::vector<int32_t> pf_items;  // prefill work records (kPfItem ints per row pass)
@@ -223,10 +229,28 @@ mtn_status hip_fail(mtn_pool *p, hipError_t e, const char *where) noexcept {
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Bytes of one (layer, block, kv head) region: K tile + V^T tile of 16 x D
-// elements, or for fp8 the code tiles plus 32 exponent bytes, padded to 128.
+// elements, or for fp8 the code tiles plus 32 exponent bytes, padded to 128;
+// int8: the code tiles.
 int64_t kv_head_stride(const mtn_pool_config *c) {
     if (c->kv_dtype == MTN_FP8_E4M3) return fp8_head_stride(c->head_dim);
+    if (c->kv_dtype == MTN_INT8_BLOCK) return 2 * (int64_t)kBlock * c->head_dim;
     return 2 * (int64_t)kBlock * c->head_dim * (c->kv_dtype == MTN_BF16 ? 2 : 4);
+}
+
+// ... of one (layer, block): every head's region, int8: and its two scales,
+// padded to 128 bytes.
+int64_t kv_block_stride(const mtn_pool_config *c) {
+    if (c->kv_dtype == MTN_INT8_BLOCK)
+        return (c->n_kv_heads * (kv_head_stride(c) + 8) + 127) / 128 * 128;
+    return c->n_kv_heads * kv_head_stride(c);
+}
+// int8: bytes of one tail (the rows of an open block, bf16, of every layer),
+// and where the tails begin in a buffer, behind the blocks.
+int64_t tail_stride(const mtn_pool_config *c) {
+    return (int64_t)c->n_layers * c->n_kv_heads * 2 * kBlock * c->head_dim * 2;
+}
+int64_t tails_offset(const mtn_pool_config *c) {
+    return ceil_div(kv_block_stride(c) * c->n_blocks * c->n_layers, 256) * 256;
 }
 
 mtn_status validate(const mtn_pool_config *c) {
@@ -247,6 +271,8 @@ mtn_status validate(const mtn_pool_config *c) {
     if (c->kv_dtype == MTN_FP8_E4M3) {
         // E4M3 codes in the pool, bf16 queries / keys / values / outputs
         if (c->io_dtype != MTN_BF16 || c->head_dim != 128) return MTN_ERR_UNSUPPORTED;
+    } else if (c->kv_dtype == MTN_INT8_BLOCK) {
+        if (c->io_dtype != MTN_BF16) return MTN_ERR_UNSUPPORTED;
     } else {
         if (c->kv_dtype != MTN_F32 && c->kv_dtype != MTN_BF16) return MTN_ERR_INVALID_ARG;
         if (c->io_dtype != c->kv_dtype) return MTN_ERR_UNSUPPORTED;
@@ -276,6 +302,15 @@ inline void logical_slot(const mtn_pool *P, int64_t p, int32_t *lb, int32_t *off
     int64_t sigma = P->unbounded ? p : (p - P->S) % P->R;
     *lb = P->nsb + (int32_t)(sigma / kBlock);
     *off = (int32_t)(sigma % kBlock);
+}
+
+TailView tails(const mtn_pool *P) {
+    return P->int8 ? TailView{P->kv + tails_offset(&P->cfg), tail_stride(&P->cfg)} : TailView{nullptr, 0};
+}
+// int8: rows of a session's open block (0 where its last block is complete)
+int32_t open_rows(const mtn_pool *P, int64_t len) {
+    if (len < P->S) return (int32_t)(len % kBlock);
+    return len == P->S ? 0 : (int32_t)((len - P->S) % kBlock);
 }
 
 // Number of not-yet-assigned logical blocks session `sid` touches when
@@ -387,7 +422,7 @@ struct PfCost {
     double start, stage;
 };
 PfCost pf_cost(const mtn_pool *P, int64_t rpp) {
-    const bool wide = rpp > 128, fp8 = P->cfg.kv_dtype == MTN_FP8_E4M3;
+    const bool wide = rpp > 128, fp8 = P->cfg.kv_dtype == MTN_FP8_E4M3 || P->int8;
     if (P->cfg.kv_dtype == MTN_F32) return P->cfg.head_dim == 64 ? PfCost{6.2, 0.71} : PfCost{9.5, 1.17};
     if (P->cfg.head_dim == 64) return wide ? PfCost{8.0, 0.73} : PfCost{7.0, 0.39};
     return wide ? PfCost{10.5, fp8 ? 0.85 : 0.57} : PfCost{9.0, fp8 ? 0.97 : 0.46};
@@ -492,7 +527,8 @@ void plan_prefill(mtn_pool *P) {
                 (int32_t)keys_seen(P, pos0 + p * rpp / P->G, pos0 + last / P->G),
                 (int32_t)P->pf_order.size());
             const int32_t rec[kPfItem] = {(int32_t)p, t0, nt, P->seq_sid[i],
-                                          (int32_t)pos0, P->tok_row[t0], 0, 0};
+                                          (int32_t)pos0, P->tok_row[t0],
+                                          P->int8 ? (int32_t)P->seq_tail[i] : 0, 0};
             P->pf_items.insert(P->pf_items.end(), rec, rec + kPfItem);
         }
     }
@@ -536,6 +572,24 @@ int32_t page_lb(const mtn_pool *P, int32_t sid, int32_t i) {
     return i < n ? i : P->nsb + (i - n);
 }
 
+// int8: tail slots (2 * session + which of its two) of one buffer into another's
+mtn_status copy_tails(mtn_pool *P, const TailView &from, const TailView &to,
+                      const std::vector<std::pair<int32_t, int32_t>> &slots, hipStream_t s) {
+    TailArgs a;
+    a.from = from.base;
+    a.to = to.base;
+    a.stride = from.stride;
+    for (size_t i = 0; i < slots.size(); i += kTailCopies) {
+        a.n = (int32_t)std::min<size_t>(kTailCopies, slots.size() - i);
+        for (int32_t j = 0; j < a.n; ++j) {
+            a.src[j] = slots[i + j].first;
+            a.dst[j] = slots[i + j].second;
+        }
+        HIP_TRY(P, launch_copy_tails(a, s));
+    }
+    return MTN_OK;
+}
+
 // The fork's device work: the source's pages into the blocks that the copies'
 // table rows name, and those rows.
 mtn_status fork_pages(mtn_pool *P, int32_t src, const std::vector<int32_t> &sids, hipStream_t s) {
@@ -560,6 +614,11 @@ mtn_status fork_pages(mtn_pool *P, int32_t src, const std::vector<int32_t> &sids
                         P->table[(size_t)a.sid[c] * P->row_len + page_lb(P, src, a.first + i)];
             HIP_TRY(P, launch_fork(a, P->cfg.n_layers, s));
         }
+    }
+    if (P->int8 && open_rows(P, P->len[src])) {
+        std::vector<std::pair<int32_t, int32_t>> slots;
+        for (const int32_t c : sids) slots.emplace_back(2 * src + P->tail[src], 2 * c + P->tail[src]);
+        return copy_tails(P, tails(P), tails(P), slots, s);
     }
     return MTN_OK;
 }
@@ -606,6 +665,7 @@ mtn_status plan_begin(mtn_pool *P, int32_t n_seq, const int32_t *sids, const int
     P->seq_ntok.assign(n_tok, n_tok + n_seq);
     P->seq_first.resize(n_seq);
     P->seq_pos0.resize(n_seq);
+    P->seq_tail.resize(n_seq);
     P->tok_sid.resize(T);
     P->tok_pos.resize(T);
     P->tok_row.resize(T);
@@ -621,6 +681,7 @@ mtn_status plan_begin(mtn_pool *P, int32_t n_seq, const int32_t *sids, const int
         P->seq_first[i] = t;
         P->seq_pos0[i] = P->len[sid];
         P->max_ntok = std::max(P->max_ntok, n_tok[i]);
+        P->seq_tail[i] = P->tail[sid];
         for (int32_t j = 0; j < n_tok[i]; ++j, ++t) {
             int64_t pos = P->len[sid] + j;
             int32_t lb, off;
@@ -638,6 +699,7 @@ mtn_status plan_begin(mtn_pool *P, int32_t n_seq, const int32_t *sids, const int
             P->tok_row[t] = rows ? rows[i] : t;
             P->tok_block[t] = row[lb];
             P->tok_off[t] = off;
+            if (off == 0) P->seq_tail[i] = P->tail[sid] ^ 1;  // the plan begins a block
         }
     }
     if (P->unbounded) P->reserved = P->assigned;
@@ -698,6 +760,14 @@ mtn_status plan_begin(mtn_pool *P, int32_t n_seq, const int32_t *sids, const int
     put(P->tok_row.data(), T);
     put(P->tok_block.data(), T);
     put(P->tok_off.data(), T);
+    if (P->int8)  // with the tail that each token's block uses
+        for (int32_t i = 0, tt = 0; i < n_seq; ++i) {
+            int32_t slot = P->tail[sids[i]];
+            for (int32_t j = 0; j < n_tok[i]; ++j, ++tt) {
+                if (P->tok_off[tt] == 0) slot = P->seq_tail[i];
+                h[o - T + tt] |= slot << 8;
+            }
+        }
     put(P->upd_idx.data(), U);
     put(P->upd_val.data(), U);
     while (o < o_items) h[o++] = 0;
@@ -749,7 +819,10 @@ mtn_status plan_commit(mtn_pool *P) {
     if (!P->host_only)
         for (auto d : P->layer_done)
             if (!d) return fail(P, MTN_ERR_BAD_STATE, "commit before every layer was appended");
-    for (int32_t i = 0; i < P->n_seq; ++i) P->len[P->seq_sid[i]] += P->seq_ntok[i];
+    for (int32_t i = 0; i < P->n_seq; ++i) {
+        P->len[P->seq_sid[i]] += P->seq_ntok[i];
+        P->tail[P->seq_sid[i]] = P->seq_tail[i];
+    }
     P->plan_open = false;
     return MTN_OK;
 }
@@ -853,6 +926,9 @@ mtn_status append_impl(mtn_pool *P, int32_t layer, const void *k, const void *v,
     if (st) return st;
     if (P->cfg.kv_dtype == MTN_FP8_E4M3)
         HIP_TRY(P, launch_append_fp8(geom(P), P->view, layer, k, v, s));
+    else if (P->int8)
+        HIP_TRY(P, launch_append_i8(geom(P), P->view, layer, k, v, tails(P), P->d_run_tok0,
+                                    P->d_run_len, (int32_t)P->run_tok0.size(), s));
     else
         HIP_TRY(P, launch_append(P->cfg.kv_dtype, geom(P), P->view, layer, k, v, P->d_run_tok0,
                                  P->d_run_len, (int32_t)P->run_tok0.size(), s));
@@ -898,7 +974,7 @@ AttnArgs attn_args(mtn_pool *P, int32_t layer, const void *q, void *out, float *
 // mtn_pool_set_decode_kernel can force either kernel where it exists, the MFMA
 // one at head dim 128 only.
 bool use_mfma(const mtn_pool *P, int64_t units) {
-    if (P->cfg.kv_dtype == MTN_FP8_E4M3) return true;
+    if (P->cfg.kv_dtype == MTN_FP8_E4M3 || P->int8) return true;
     if (P->cfg.kv_dtype != MTN_BF16 || !attn_mfma_bf16_supported(P->cfg.head_dim, P->G))
         return false;
     if (P->decode_kernel) return P->decode_kernel == 2;
@@ -981,6 +1057,8 @@ mtn_status decode_impl(mtn_pool *P, int32_t layer, const void *q, void *out, flo
     }
     if (P->cfg.kv_dtype == MTN_FP8_E4M3)
         HIP_TRY(P, launch_attn_fp8(a, s));
+    else if (P->int8)
+        HIP_TRY(P, launch_attn_i8(a, tails(P), s));
     else if (use_mfma(P, (int64_t)P->T * P->cfg.n_kv_heads))
         HIP_TRY(P, launch_attn_mfma_bf16(a, s));
     else
@@ -1044,7 +1122,7 @@ mtn_status prefill_impl(mtn_pool *P, int32_t layer, const void *q, void *out, fl
         HIP_TRY(P, launch_prefill_f32(a, P->d_pf_items, n_items, s));
     else
         HIP_TRY(P, launch_prefill_mfma(P->cfg.kv_dtype, a, P->d_pf_items, n_items, P->pf_rows,
-                                       P->d_zero, s));
+                                       P->d_zero, tails(P), s));
     st = timing_end(P, 1, e0, s);
     if (st) return st;
     if (k_new) P->layer_done[layer] = 1;
@@ -1149,8 +1227,9 @@ mtn_status mtn_pool_required_bytes(const mtn_pool_config *cfg, size_t *kv_bytes)
     mtn_status st = validate(cfg);
     if (st) return st;
     if (!kv_bytes) return MTN_ERR_INVALID_ARG;
-    size_t per_block = (size_t)cfg->n_kv_heads * (size_t)kv_head_stride(cfg);
-    *kv_bytes = per_block * (size_t)cfg->n_blocks * (size_t)cfg->n_layers;
+    *kv_bytes = (size_t)kv_block_stride(cfg) * (size_t)cfg->n_blocks * (size_t)cfg->n_layers;
+    if (cfg->kv_dtype == MTN_INT8_BLOCK)
+        *kv_bytes = (size_t)tails_offset(cfg) + 2 * (size_t)cfg->max_sessions * (size_t)tail_stride(cfg);
     return MTN_OK;
 }
 
@@ -1164,8 +1243,9 @@ mtn_status mtn_pool_create(const mtn_pool_config *cfg, void *kv_dev, size_t kv_b
     if (!host_only) {
         if (!kv_dev || kv_bytes < need || ((uintptr_t)kv_dev & 255)) return MTN_ERR_INVALID_ARG;
         const int g = cfg->n_q_heads / cfg->n_kv_heads;
-        if (cfg->kv_dtype == MTN_FP8_E4M3 ? !attn_fp8_supported(cfg->head_dim, g)
-                                          : !attn_valu_supported(cfg->kv_dtype, cfg->head_dim, g))
+        if (cfg->kv_dtype == MTN_FP8_E4M3     ? !attn_fp8_supported(cfg->head_dim, g)
+            : cfg->kv_dtype == MTN_INT8_BLOCK ? !attn_i8_supported(cfg->head_dim, g)
+                                              : !attn_valu_supported(cfg->kv_dtype, cfg->head_dim, g))
             return MTN_ERR_UNSUPPORTED;
     }
     mtn_pool *P = new (std::nothrow) mtn_pool();
@@ -1194,6 +1274,7 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
     P->cfg = *cfg;
     P->host_only = host_only;
     P->unbounded = cfg->window == MTN_WINDOW_UNBOUNDED;
+    P->int8 = cfg->kv_dtype == MTN_INT8_BLOCK;
     P->G = cfg->n_q_heads / cfg->n_kv_heads;
     P->elt = cfg->io_dtype == MTN_BF16 ? 2 : 4;  // io element size
     if (P->unbounded) {
@@ -1208,9 +1289,10 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
         P->R = (int32_t)(ceil_div((int64_t)cfg->window + cfg->max_chunk - 1, kBlock) * kBlock);
     }
     P->row_len = P->nsb + P->R / kBlock;
-    P->tile_bytes = (int64_t)kBlock * cfg->head_dim * (cfg->kv_dtype == MTN_FP8_E4M3 ? 1 : (int64_t)P->elt);
+    P->tile_bytes = (int64_t)kBlock * cfg->head_dim *
+                    (cfg->kv_dtype == MTN_FP8_E4M3 || P->int8 ? 1 : (int64_t)P->elt);
     P->head_stride = kv_head_stride(cfg);
-    P->block_stride = P->head_stride * cfg->n_kv_heads;
+    P->block_stride = kv_block_stride(cfg);
     P->layer_stride = P->block_stride * cfg->n_blocks;
     P->scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale
                                         : (float)(1.0 / std::sqrt((double)cfg->head_dim));
@@ -1220,6 +1302,7 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
     P->is_open.assign((size_t)cfg->max_sessions, 0);
     P->len.assign((size_t)cfg->max_sessions, 0);
     P->n_assigned.assign((size_t)cfg->max_sessions, 0);
+    P->tail.assign((size_t)cfg->max_sessions, 0);
     P->alloc.reset(cfg->n_blocks);
     P->max_tok = cfg->max_sessions * cfg->max_chunk;
     // the planner's per-plan vectors at their largest, so that planning
@@ -1228,6 +1311,7 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
     P->seq_ntok.reserve((size_t)cfg->max_sessions);
     P->seq_first.reserve((size_t)cfg->max_sessions);
     P->seq_pos0.reserve((size_t)cfg->max_sessions);
+    P->seq_tail.reserve((size_t)cfg->max_sessions);
     for (auto *v : {&P->tok_sid, &P->tok_pos, &P->tok_row, &P->tok_block, &P->tok_off, &P->upd_idx,
                     &P->upd_val, &P->run_tok0, &P->run_len})
         v->reserve((size_t)P->max_tok);
@@ -1298,9 +1382,11 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
         const bool fp8 = cfg->kv_dtype == MTN_FP8_E4M3;
         if (fp8)
             P->resident_mfma = n_cu * attn_fp8_resident_per_cu(P->G);
+        else if (P->int8)
+            P->resident_mfma = n_cu * attn_i8_resident_per_cu(cfg->head_dim, P->G);
         else if (cfg->kv_dtype == MTN_BF16 && attn_mfma_bf16_supported(cfg->head_dim, P->G))
             P->resident_mfma = n_cu * attn_mfma_bf16_resident_per_cu(cfg->head_dim, P->G);
-        if (!fp8)
+        if (!fp8 && !P->int8)
             P->resident_valu =
                 n_cu * std::min(4, attn_valu_resident_per_cu(cfg->kv_dtype, cfg->head_dim, P->G));
         if ((e = hipEventCreateWithFlags(&P->order_ev, hipEventDisableTiming)) != hipSuccess)
@@ -1382,6 +1468,7 @@ mtn_status mtn_session_open(mtn_pool *P, int32_t *sid_out) {
         P->is_open[sid] = 1;
         P->len[sid] = 0;
         P->n_assigned[sid] = 0;
+        P->tail[sid] = 0;
         P->n_open++;
         *sid_out = sid;
         return MTN_OK;
@@ -1459,6 +1546,7 @@ mtn_status mtn_session_fork(mtn_pool *P, int32_t sid, int32_t n_copies, int32_t 
             P->is_open[c] = 1;
             P->len[c] = P->len[sid];
             P->n_assigned[c] = (int32_t)pages;
+            P->tail[c] = P->tail[sid];
         }
         P->n_open += n_copies;
         P->assigned += pages * n_copies;
@@ -1524,6 +1612,15 @@ mtn_status mtn_pool_resize(mtn_pool *P, int64_t n_blocks, void *kv_dev, size_t k
                 return e;
             };
             HIP_TRY(P, each([&] { return launch_move(a, P->cfg.n_layers, (hipStream_t)stream); }));
+            if (P->int8) {
+                std::vector<std::pair<int32_t, int32_t>> slots;
+                for (const MoveSession &m : moves)
+                    if (open_rows(P, P->len[m.sid]))
+                        slots.emplace_back(2 * m.sid + P->tail[m.sid], 2 * m.sid + P->tail[m.sid]);
+                const TailView to{(uint8_t *)kv_dev + tails_offset(&cfg), tail_stride(&cfg)};
+                st = copy_tails(P, tails(P), to, slots, (hipStream_t)stream);
+                if (st) return st;
+            }
             const hipError_t e = each([&] { return launch_move_table(a, (hipStream_t)stream); });
             if (e != hipSuccess) {  // back to the tables of the old buffer
                 (void)hipStreamSynchronize((hipStream_t)stream);
@@ -1757,11 +1854,16 @@ mtn_status mtn_debug_poison_dead(mtn_pool *P, void *stream) {
         if (P->plan_open) return fail(P, MTN_ERR_BAD_STATE, "plan open");
         // live[b] bit o set <=> slot o of block b holds a retained position
         std::vector<uint16_t> live((size_t)P->cfg.n_blocks, 0);
+        std::vector<uint8_t> rows(P->int8 ? 2 * (size_t)P->cfg.max_sessions : 0, 0);  // ... of every tail
         for (int32_t sid = 0; sid < P->cfg.max_sessions; ++sid) {
             if (!P->is_open[sid]) continue;
             const int32_t *row = &P->table[(size_t)sid * P->row_len];
             int64_t L = P->len[sid];
             int64_t lo = P->unbounded ? 0 : std::max<int64_t>(P->S, L - P->W);
+            if (P->int8) {  // the open block's positions lie in the tail, not in their slots
+                rows[2 * sid + P->tail[sid]] = (uint8_t)open_rows(P, L);
+                L -= open_rows(P, L);
+            }
             auto mark = [&](int64_t p) {
                 int32_t lb, off;
                 logical_slot(P, p, &lb, &off);
@@ -1772,11 +1874,16 @@ mtn_status mtn_debug_poison_dead(mtn_pool *P, void *stream) {
         }
         hipStream_t s = (hipStream_t)stream;
         uint16_t *d_live = nullptr;
-        HIP_TRY(P, hipMalloc(&d_live, sizeof(uint16_t) * live.size()));
-        HIP_TRY(P, hipMemcpy(d_live, live.data(), sizeof(uint16_t) * live.size(),
-                             hipMemcpyHostToDevice));
+        const size_t live_bytes = sizeof(uint16_t) * live.size();
+        HIP_TRY(P, hipMalloc(&d_live, live_bytes + rows.size()));
+        HIP_TRY(P, hipMemcpy(d_live, live.data(), live_bytes, hipMemcpyHostToDevice));
+        uint8_t *d_rows = (uint8_t *)d_live + live_bytes;
+        if (P->int8) HIP_TRY(P, hipMemcpy(d_rows, rows.data(), rows.size(), hipMemcpyHostToDevice));
         if (P->cfg.kv_dtype == MTN_FP8_E4M3)
             HIP_TRY(P, launch_poison_fp8(geom(P), P->cfg.n_layers, P->cfg.n_blocks, d_live, s));
+        else if (P->int8)
+            HIP_TRY(P, launch_poison_i8(geom(P), tails(P), P->cfg.n_layers, P->cfg.n_blocks,
+                                        (int32_t)rows.size(), d_live, d_rows, s));
         else
             HIP_TRY(P, launch_poison(P->cfg.kv_dtype, geom(P), P->cfg.n_layers, P->cfg.n_blocks, d_live, s));
         HIP_TRY(P, hipStreamSynchronize(s));
@@ -1801,8 +1908,8 @@ mtn_status mtn_pool_set_decode_kernel(mtn_pool *P, int32_t kind) {
         if (kind < 0 || kind > 2) return fail(P, MTN_ERR_INVALID_ARG, "kind must be 0, 1 or 2");
         if (P->plan_open) return fail(P, MTN_ERR_BAD_STATE, "plan open");
         const mtn_pool_config &c = P->cfg;
-        if (kind == 1 && c.kv_dtype == MTN_FP8_E4M3)
-            return fail(P, MTN_ERR_UNSUPPORTED, "the FP8 cache has no vector decode kernel");
+        if (kind == 1 && (c.kv_dtype == MTN_FP8_E4M3 || P->int8))
+            return fail(P, MTN_ERR_UNSUPPORTED, "8-bit caches have no vector decode kernel");
         if (kind == 2 && c.kv_dtype == MTN_F32)
             return fail(P, MTN_ERR_UNSUPPORTED, "fp32 pools have no matrix decode kernel");
         if (kind == 2 && (c.head_dim != 128 || !attn_mfma_bf16_supported(c.head_dim, P->G)))

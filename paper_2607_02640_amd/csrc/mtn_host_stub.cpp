@@ -22,7 +22,7 @@ hipError_t launch_merge(int, const AttnArgs &, hipStream_t) { return hipErrorNot
 int prefill_rows_per_pass() { return 256; }
 bool prefill_pass_rows_valid(int rows) { return rows == 128 || rows == 256; }
 hipError_t launch_prefill_mfma(int, const AttnArgs &, const int32_t *, int32_t, int32_t,
-                               const uint8_t *, hipStream_t) {
+                               const uint8_t *, const TailView &, hipStream_t) {
     return hipErrorNotSupported;
 }
 int prefill_f32_rows_per_pass() { return 64; }
@@ -52,6 +52,18 @@ hipError_t launch_attn_fp8(const AttnArgs &, hipStream_t) { return hipErrorNotSu
 hipError_t launch_poison_fp8(const PoolGeom &, int32_t, int64_t, const uint16_t *, hipStream_t) {
     return hipErrorNotSupported;
 }
+bool attn_i8_supported(int d, int g) { return (d == 128 || d == 64) && group_ok(g); }
+int attn_i8_resident_per_cu(int, int) { return 1; }
+hipError_t launch_append_i8(const PoolGeom &, const PlanView &, int32_t, const void *, const void *,
+                            const TailView &, const int32_t *, const int32_t *, int32_t, hipStream_t) {
+    return hipErrorNotSupported;
+}
+hipError_t launch_attn_i8(const AttnArgs &, const TailView &, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_poison_i8(const PoolGeom &, const TailView &, int32_t, int64_t, int32_t,
+                            const uint16_t *, const uint8_t *, hipStream_t) {
+    return hipErrorNotSupported;
+}
+hipError_t launch_copy_tails(const TailArgs &, hipStream_t) { return hipErrorNotSupported; }
 bool attn_mfma_bf16_supported(int d, int g) { return (d == 128 || d == 64) && group_ok(g); }
 int attn_mfma_bf16_resident_per_cu(int, int) { return 1; }
 hipError_t launch_attn_mfma_bf16(const AttnArgs &, hipStream_t) { return hipErrorNotSupported; }
@@ -62,7 +74,7 @@ int attn_valu_resident_per_cu(int, int, int) { return 1; }
 int attn_valu_groups(int) { return 1; }
 int attn_mfma_groups(int) { return 4; }
 bool prefill_mfma_supported(int dtype, int d, int g) {
-    return (((dtype == 0 || dtype == 1) && (d == 128 || d == 64)) || (dtype == 2 && d == 128)) &&
+    return (((dtype == 0 || dtype == 1 || dtype == 3) && (d == 128 || d == 64)) || (dtype == 2 && d == 128)) &&
            group_ok(g);
 }
 

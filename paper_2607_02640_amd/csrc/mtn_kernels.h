@@ -60,7 +60,18 @@ struct AttnArgs {
     const void *v_new;
 };
 
-// dtype codes match the public MTN_F32 / MTN_BF16 / MTN_FP8_E4M3
+// Tails of an int8 pool (the rows of every session's open block): per (session,
+// one of two), `stride` bytes: [layer][kv head]{K [16][D], V [16][D] bf16}.
+struct TailView {
+    uint8_t *base;
+    int64_t stride;
+};
+struct I8Args {
+    AttnArgs a;
+    TailView tails;
+};
+
+// dtype codes match the public MTN_F32 / MTN_BF16 / MTN_FP8_E4M3 / MTN_INT8_BLOCK
 // src non-null: pinned host words, first copied to dst (both 16-byte aligned,
 // whole 16-byte vectors allocated); the other arrays may lie in src.
 hipError_t launch_plan_apply(const int32_t *src, int32_t *dst, int32_t n_words,
@@ -80,10 +91,11 @@ hipError_t launch_append(int dtype, const PoolGeom &g, const PlanView &p, int32_
 hipError_t launch_attn_valu(int dtype, const AttnArgs &a, hipStream_t s);
 hipError_t launch_merge(int dtype, const AttnArgs &a, hipStream_t s);
 
-// MFMA chunk-prefill attention (bf16 pool, D = 128 or 64; fp8 pool, D = 128): one
+// MFMA chunk-prefill attention (bf16 and int8 pools, D = 128 or 64; fp8 pool, D = 128): one
 // workgroup per (sequence, row pass, kv head, key segment of a.n_split).  items: n_items records of kPfItem int32 (32-byte
 // aligned), one per row pass: {pass, first planned token t0, tokens, session
-// id, position of t0, io row of t0, 0, 0}; token t0 + j of the sequence uses
+// id, position of t0, io row of t0, tail (int8 pools: which of the session's two
+// holds its open block once the plan is appended), 0}; token t0 + j of the sequence uses
 // io row (row of t0) + j (multi-token plans always do); pass p covers the
 // sequence's query rows [p, p + 1) * pass_rows (rows are token * G + group
 // head).  pass_rows: prefill_rows_per_pass() or, to spread few sequences over
@@ -96,7 +108,8 @@ constexpr int kPfItem = 8;
 int prefill_rows_per_pass();
 bool prefill_pass_rows_valid(int rows);
 hipError_t launch_prefill_mfma(int dtype, const AttnArgs &a, const int32_t *items, int32_t n_items,
-                               int32_t pass_rows, const uint8_t *zero_page, hipStream_t s);
+                               int32_t pass_rows, const uint8_t *zero_page, const TailView &tails,
+                               hipStream_t s);
 
 // The same over fp32 pools (D = 64 or 128), a.zero_page the zero page:
 // passes of prefill_f32_rows_per_pass() rows.
@@ -145,6 +158,17 @@ struct MoveArgs {
 hipError_t launch_move(const MoveArgs &a, int32_t n_layers, hipStream_t s);
 hipError_t launch_move_table(const MoveArgs &a, hipStream_t s);
 
+// Tails: slot src[i] of one buffer's tails to slot dst[i] of another's (or the same's).
+constexpr int kTailCopies = 480;
+struct TailArgs {
+    const uint8_t *from;
+    uint8_t *to;
+    int64_t stride;  // bytes of a slot
+    int32_t n;
+    int32_t src[kTailCopies], dst[kTailCopies];
+};
+hipError_t launch_copy_tails(const TailArgs &a, hipStream_t s);
+
 // The library's static device workspace for split partials (a file-scope
 // array, no allocation): its address on the current device and its size in
 // floats.
@@ -167,6 +191,19 @@ hipError_t launch_poison_fp8(const PoolGeom &g, int32_t n_layers, int64_t n_bloc
 bool attn_mfma_bf16_supported(int d, int g);
 int attn_mfma_bf16_resident_per_cu(int d, int g);
 hipError_t launch_attn_mfma_bf16(const AttnArgs &a, hipStream_t s);
+
+// int8 KV cache (bf16 io, D = 128 or 64): tok_off of its plans holds the slot
+// in bits 0 .. 7 and which of the session's tails the token's block uses (while
+// open) in bit 8.
+bool attn_i8_supported(int d, int g);
+int attn_i8_resident_per_cu(int d, int g);
+hipError_t launch_append_i8(const PoolGeom &g, const PlanView &p, int32_t layer, const void *k,
+                            const void *v, const TailView &tails, const int32_t *run_tok0,
+                            const int32_t *run_len, int32_t n_runs, hipStream_t s);
+hipError_t launch_attn_i8(const AttnArgs &a, const TailView &tails, hipStream_t s);
+hipError_t launch_poison_i8(const PoolGeom &g, const TailView &tails, int32_t n_layers,
+                            int64_t n_blocks, int32_t n_tails, const uint16_t *live_mask,
+                            const uint8_t *tail_rows, hipStream_t s);
 
 bool attn_valu_supported(int dtype, int d, int g);
 // workgroups of the vector attention kernel resident per CU (occupancy query)

@@ -827,6 +827,7 @@ struct PfArgs {
     const int32_t *items;      // kPfItem-int records, one per (sequence, row pass)
     const uint8_t *zero_page;  // 16 KiB of zeros: the DMA source of absent blocks
     int32_t pass_rows;         // query rows per pass: 128 or kPfRowsPerPass
+    TailView tails;            // int8 pools
 };
 
 // LDS layout of one stage: K tiles of blocks 0, 1 (the 16-byte chunks of a
@@ -920,21 +921,74 @@ __device__ __forceinline__ void f8_stage_to_bf16(const uint8_t *src, uint8_t *ds
     }
 }
 
+// Int8 codes (four bytes, signed) as bf16, exact.
+__device__ __forceinline__ uint2 i8_bf16x4(uint32_t w) {
+    const float f0 = (float)(int8_t)w, f1 = (float)(int8_t)(w >> 8);
+    const float f2 = (float)(int8_t)(w >> 16), f3 = (float)(int8_t)(w >> 24);
+    return make_uint2(__builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u),
+                      __builtin_amdgcn_perm(__float_as_uint(f3), __float_as_uint(f2), 0x07060302u));
+}
+// ... eight K codes (stored plus 128) of a row
+__device__ __forceinline__ uint4 i8_keys(const uint2 &c) {
+    const uint2 a = i8_bf16x4(c.x ^ 0x80808080u), b = i8_bf16x4(c.y ^ 0x80808080u);
+    return make_uint4(a.x, a.y, b.x, b.y);
+}
+// An int8 stage (two regions of `blk` bytes: K codes, V codes in key quads, 16
+// bytes with the scales) -> the bf16 stage layout, codes as they are: the scales
+// are applied to scores and probabilities.  Block tail_b (or none) comes from
+// `tail`, K [16][D] and V [16][D] bf16.  512 threads, 256 per block: K dims 8 hc .. + 7
+// of a key, and V dims 2 dp, 2 dp + 1 of a key quad, D = 64 one of the two.
+template <int D>
+__device__ __forceinline__ void i8_stage_to_bf16(const uint8_t *src, int blk, uint8_t *dst, int tid, int tail_b,
+                                                 const uint8_t *tail) {
+    const int b = tid >> 8, u = tid & 255;
+    const bool from_tail = b == tail_b;
+    src += b * blk;
+    if (D == 128 || u < 128) {
+        const int key = u / (D / 8), hc = u % (D / 8);
+        *(uint4 *)(dst + PfLds<D>::k(b, key, hc)) =
+            from_tail ? ((const uint4 *)(tail + key * 2 * D))[hc] : i8_keys(((const uint2 *)(src + key * D))[hc]);
+    }
+    if (D == 128 || u >= 128) {
+        const int kg = (u / (D / 2)) & 3, dp = u % (D / 2);
+        uint2 v[2];
+        if (from_tail) {
+            const uint32_t *r = (const uint32_t *)(tail + 32 * D) + 4 * kg * (D / 2) + dp;
+            const uint32_t r0 = r[0], r1 = r[D / 2], r2 = r[D], r3 = r[D / 2 * 3];
+            v[0] = make_uint2(__builtin_amdgcn_perm(r1, r0, 0x05040100u), __builtin_amdgcn_perm(r3, r2, 0x05040100u));
+            v[1] = make_uint2(__builtin_amdgcn_perm(r1, r0, 0x07060302u), __builtin_amdgcn_perm(r3, r2, 0x07060302u));
+        } else {
+            const uint2 c = ((const uint2 *)(src + kBlock * D))[kg * (D / 2) + dp];
+            v[0] = i8_bf16x4(c.x);
+            v[1] = i8_bf16x4(c.y);
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            *(uint2 *)(dst + PfLds<D>::v16(b, 2 * dp + x, kg >> 1) + (kg & 1) * 8) = v[x];
+    }
+}
+
+// What the pool holds: bf16 rows, E4M3 codes, or int8 codes.
+enum KvForm { kKvBf16, kKvF8, kKvI8 };
+
 // F8: the pool holds E4M3 codes.  Each stage then lands as two kF8Read-byte
 // regions (per block four 1 KiB DMA instructions plus the 32 exponent
 // bytes), and every stage is converted into one of two bf16 stage buffers (a
 // second barrier) before the same MFMA stage body runs on it.
-template <int D, int G, bool F8, bool RF>
+template <int D, int G, int FORM, bool RF>
 __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
     using Lds = PfLds<D>;
+    constexpr bool F8 = FORM == kKvF8, I8 = FORM == kKvI8, Q8 = F8 || I8;
     static_assert(D == 128 || (D == 64 && !F8), "head dims with a stage layout");
+    constexpr int kI8Codes = 2 * kBlock * D, kI8Blk = kI8Codes + 16;  // codes of a (block, head); with its scales
     constexpr int ND = D / 32;   // 32-wide slices of d (QK MFMAs per key row)
     constexpr int NT16 = D / 16; // 16-wide tiles of d (PV MFMAs)
-    constexpr int SB = F8 ? 2 * kF8Read : Lds::kStage;  // bytes of a ring stage
+    constexpr int SB = F8 ? 2 * kF8Read : I8 ? 2 * kI8Blk : Lds::kStage;  // bytes of a ring stage
     static_assert(kPfStages >= 3 && kPfStages <= 8, "ring depth (the DMA waits count at most 63)");
     static_assert(kPfEarly >= 1 && kPfEarly <= kPfStages - 1, "early stages are ring prologue stages");
     __shared__ __attribute__((aligned(16))) uint8_t ring[kPfStages][SB];
-    __shared__ __attribute__((aligned(16))) uint8_t bfs[F8 ? 2 : 1][F8 ? Lds::kStage : 16];
+    __shared__ __attribute__((aligned(16))) uint8_t bfs[Q8 ? 2 : 1][Q8 ? Lds::kStage : 16];
+    __shared__ __attribute__((aligned(16))) uint8_t tailb[I8 ? 2 * Lds::kTile : 16];  // the open block's rows
     const AttnArgs &a = pa.a;
     const PoolGeom &g = a.g;
     // one workgroup per (sequence, row pass, kv head, key segment): a long
@@ -992,6 +1046,21 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
     const int n_stages = seg_begin(seg + 1, ns, all_stages) - st0;
     const int vb0 = 2 * st0;
     const int seg_nvb = min(nvb - vb0, 2 * n_stages);  // blocks of the segment
+    // int8: the union's last block, if the plan leaves it open, lies in the
+    // session's tail: its number in the segment, or -1
+    int tail_v = -1;
+    const uint8_t *tail_rows = nullptr;
+    if constexpr (I8) {
+        const int lp = pos0 + ntok - 1;  // the plan's last position
+        const int lo = (lp < g.n_sink ? lp : lp - g.n_sink) % kBlock;
+        const int rows = lp < g.n_sink ? min(kBlock, g.n_sink - (lp - lo)) : kBlock;
+        if (lo + 1 < rows && tq_max >= lp - lo && nvb - 1 >= vb0 && nvb - 1 - vb0 < seg_nvb) {
+            tail_v = nvb - 1 - vb0;
+            tail_rows = pa.tails.base + ((int64_t)sid * 2 + scalar_ld(rec, 6)) * pa.tails.stride +
+                        ((int64_t)a.layer * g.hkv + kvh) * (64 * D);
+        }
+    }
+    const uint32_t i8_scale_off = (uint32_t)((g.hkv - kvh) * kI8Codes + (kvh >> 1) * 16);  // from the head's codes
 
     auto vblock = [&](int v) {
         v += vb0;
@@ -1027,8 +1096,9 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
     // F8: 4 for the K and V codes, one 2-lane instruction for the 32 exponent
     // bytes -- and DMA wave i issues those k = (i >> 1) + (DW / 2) m, m < NPW.
     constexpr int NKI = Lds::kTile / 1024;    // ... of a K (or V^T) tile
-    constexpr int NDI = F8 ? 5 : 2 * NKI;  // DMA instructions per block
-    constexpr int DW = F8 ? 2 : MTN_PF_DMA_WAVES;
+    constexpr int NCI = I8 ? kI8Codes / 1024 : 4;  // ... of the codes of a block
+    constexpr int NDI = Q8 ? NCI + 1 : 2 * NKI;  // DMA instructions per block
+    constexpr int DW = Q8 ? 2 : MTN_PF_DMA_WAVES;
     constexpr int NPW = NDI / (DW / 2);  // DMA instructions per DMA wave per stage
     static_assert(DW >= 2 && NPW * (DW / 2) == NDI, "DMA split");
     // The DMA waves are waves 2 and 3: with waves w and w + 4 sharing a SIMD,
@@ -1048,6 +1118,9 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         if constexpr (F8) {
             dsrc[m] = j < 4 ? j * 1024 + lane * 16 : kF8Exp + (lane & 1) * 16;
             ddst[m] = db * kF8Read + (j < 4 ? j * 1024 : kF8Exp);
+        } else if constexpr (I8) {
+            dsrc[m] = j * 1024 + lane * 16;  // (the scales' offset: issue_block)
+            ddst[m] = db * kI8Blk + j * 1024;
         } else {
             const int off = j < NKI ? db * Lds::kTile + j * 1024
                                     : (2 + db) * Lds::kTile + (j - NKI) * 1024;
@@ -1082,6 +1155,8 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 // one query head per kv head the fp8 kernel otherwise spills
                 // it, and the reload's wait also drains the DMA ring
                 if (lane < 2) dma16_s(kF8Exp + (lane & 1) * 16, src, dst + ddst[m]);
+            } else if (I8 && m == NPW - 1) {
+                if (lane < 1) dma16_s(ph >= 0 ? i8_scale_off : 0u, src, dst + ddst[m]);
             } else {
                 dma16_s(dsrc[m], src, dst + ddst[m]);
             }
@@ -1226,10 +1301,10 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         // So does D = 64, whose reference moves too often for the shift to pay
         // (chunks of 64 sessions over 2000 keys 260 us a layer call of four with
         // it, 253 without; 4000 causal tokens 138 and 132).
-        constexpr bool kShift = !F8 && D == 128;
+        constexpr bool kShift = !Q8 && D == 128;
         float msh[kPfTpw], thr[kPfTpw];
         f32x4_t csh[kPfTpw];  // {-msh} x 4, kept so the QK start needs no moves
-        constexpr bool kMfmaSum = !F8 && D == 128;
+        constexpr bool kMfmaSum = !Q8 && D == 128;
         f32x4_t l_i[kPfTpw];
         float ls[kPfTpw];
         int tq_i[kPfTpw];
@@ -1265,6 +1340,9 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         }
         uint4 qx[kPfTpw][ND], qy[kPfTpw][ND];  // dims d0 .. d0 + 7 and their partners d0 ^ (D / 2)
         float4 qc[kPfTpw][ND / 2][4];          // (cos, sin) of dims (d0 % (D / 2)) .. + 7
+        uint4 tail_part = make_uint4(0, 0, 0, 0);  // this thread's 16 bytes of the open block
+        if constexpr (I8)
+            if (tail_v >= 0 && tid < 4 * D) tail_part = ((const uint4 *)tail_rows)[tid];
         AppBatch ab;
         if (fuse && !dma_wave) app_load(aw, ab);
         __builtin_amdgcn_sched_barrier(0);  // the query loads follow at once
@@ -1351,7 +1429,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         // the four lanes of a row.
         // the bf16 stage buffer the MFMAs read for stage st
         auto stage_buf = [&](int st) -> uint8_t * {
-            if constexpr (F8)
+            if constexpr (Q8)
                 return &bfs[st & 1][0];
             else
                 return &ring[st % kPfStages][0];
@@ -1457,12 +1535,28 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         // st - 1, which both groups finished before reaching it.  The fp8
         // kernel keeps the common barrier: its conversion step is a second
         // workgroup-wide exchange per stage.
-        constexpr bool kPP = !F8;
+        constexpr bool kPP = !Q8;
+        if constexpr (I8)
+            if (tail_v >= 0 && tid < 4 * D) ((uint4 *)tailb)[tid] = tail_part;
+        // a landed stage -> bf16
+        auto convert = [&](int st) __attribute__((always_inline)) {
+            if constexpr (F8)
+                f8_stage_to_bf16(&ring[st % kPfStages][0], stage_buf(st), tid);
+            if constexpr (I8)
+                i8_stage_to_bf16<D>(&ring[st % kPfStages][0], kI8Blk, stage_buf(st), tid,
+                                    tail_v >= 0 && tail_v / 2 == st ? tail_v & 1 : -1, tailb);
+        };
+        // int8: {K, V} scale of this lane's block in stage st, from its ring slot
+        // (which the stage's own step may still read)
+        auto scales = [&](int st) __attribute__((always_inline)) {
+            const float2 x = *(const float2 *)(&ring[st % kPfStages][0] + lblk * kI8Blk + kI8Codes + 8 * (kvh & 1));
+            return 2 * st + lblk == tail_v ? make_float2(1.f, 1.f) : x;
+        };
         const bool grp_b = kPP && wv >= kPfWaves / 2;
         if (dma_wave) vm_wait<NPW * (kPfStages - (kPP ? 3 : 2))>();  // stage 0 (and 1) landed
         __syncthreads();
-        if constexpr (F8) {
-            f8_stage_to_bf16(&ring[0][0], stage_buf(0), tid);
+        if constexpr (Q8) {
+            convert(0);
             __syncthreads();
         }
         // one stage; MASKED: the stage may hold keys some row cannot see
@@ -1475,6 +1569,16 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             uint4 vf[NT16];
 #pragma unroll
             for (int dt = 0; dt < NT16; ++dt) vf[dt] = *(const uint4 *)(sm + voff + dt * 16 * 32);
+            float v_scale = 1.f;
+            if constexpr (I8) {
+                const float2 x = scales(st);
+                v_scale = x.y;
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    sa[i] *= x.x;
+                    sb[i] *= x.x;
+                }
+            }
             if constexpr (MASKED) {
                 mask_scores(nt_c, st, sa, sb);
                 uint32_t vm[4];
@@ -1495,9 +1599,9 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                     nph = phys(2 * (nst + 1) + db);
                 }
             }
-            if constexpr (F8) {
+            if constexpr (Q8) {
                 // the other bf16 buffer: its stage (st - 1) is consumed
-                f8_stage_to_bf16(&ring[(st + 1) % kPfStages][0], stage_buf(st + 1), tid);
+                convert(st + 1);
                 __syncthreads();
             }
             // K fragments of stage st + 1.  bf16: read before the max test, whose
@@ -1512,7 +1616,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                     kf[s][1] = *(const uint4 *)(nsm + koff[s] + 4 * Lds::kRow);
                 }
             };
-            if constexpr (!F8) load_kf();
+            if constexpr (!Q8) load_kf();
             // lazy reference max: lane-local test, row max only on a bump
             float m8[kPfTpw];
             bool bump = false;
@@ -1559,7 +1663,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             // stage's probabilities: in each of ND groups, one MFMA then 8 / ND
             // VALU instructions, so the exponentials run while the matrix
             // core works
-            if constexpr (F8) load_kf();
+            if constexpr (Q8) load_kf();
             f32x4_t na[kPfTpw], nb[kPfTpw];
             float p[kPfTpw][8];
             constexpr int kEpg = 8 * NT / ND;  // probabilities per group
@@ -1592,9 +1696,13 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             }
             uint4 pb[kPfTpw];
 #pragma unroll
-            for (int i = 0; i < NT; ++i)
-                pb[i] = make_uint4(pack_bf16x2(p[i][0], p[i][1]), pack_bf16x2(p[i][2], p[i][3]),
-                                   pack_bf16x2(p[i][4], p[i][5]), pack_bf16x2(p[i][6], p[i][7]));
+            for (int i = 0; i < NT; ++i) {
+                float w[8];  // probabilities, int8: times the V scale
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = I8 ? p[i][e] * v_scale : p[i][e];
+                pb[i] = make_uint4(pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]),
+                                   pack_bf16x2(w[6], w[7]));
+            }
             if (grp_b) __syncthreads();  // group B's stage barrier
             // row sums: of the bf16 probabilities by an all-ones A operand, or
             // the lane's part by vector adds
@@ -1677,6 +1785,10 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                         const int key = (kap & 15) + 4 * x;
                         if constexpr (F8)
                             k2[x] = f8_keys(*(const uint2 *)(kb + key * D + (s * 4 + lg) * 8), kb[kF8Exp + key]);
+                        else if constexpr (I8)
+                            k2[x] = 2 * st + (kap >> 4) == tail_v
+                                        ? *(const uint4 *)(tailb + key * 2 * D + (s * 4 + lg) * 16)
+                                        : i8_keys(*(const uint2 *)(kb + key * D + (s * 4 + lg) * 8));
                         else
                             k2[x] = ((const uint4 *)(kb + key * Lds::kRow))[s * 4 + lg];
                     }
@@ -1686,6 +1798,16 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 const PfBlock mb = vblock(2 * st + lblk);
                 int vlo, vhi;
                 row_slots(mb, tq_i[i], vlo, vhi);
+                const bool in_tail = I8 && 2 * st + lblk == tail_v;
+                float v_scale = 1.f;
+                if constexpr (I8) {
+                    if (!in_tail && (lblk ? ph1 : ph0) >= 0) {
+                        const float2 x = *(const float2 *)(vb + (g.hkv - kvh) * kI8Codes + 8 * kvh);
+                        s0 *= x.x;
+                        s1 *= x.x;
+                        v_scale = x.y;
+                    }
+                }
                 float sc[8], p[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -1715,8 +1837,12 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(kShift ? sc[e] : sc[e] - m_ref[i]);
-                const uint4 pb = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]),
-                                            pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+                float w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e)  // (an unseen block's scale may be NaN)
+                    w[e] = !I8 ? p[e] : lkey0 + e >= vlo && lkey0 + e < vhi ? p[e] * v_scale : 0.f;
+                const uint4 pb = make_uint4(pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]),
+                                            pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7]));
                 if constexpr (kMfmaSum)
                     l_i[i] = mfma16x16x32(make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u),
                                           pb, l_i[i]);
@@ -1745,6 +1871,17 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                             const uint2 w1 = f8_values(*(const uint32_t *)(vq + 4 * D),
                                                        *(const uint32_t *)(ve + 4));
                             v = make_uint4(w0.x, w0.y, w1.x, w1.y);
+                        } else if constexpr (I8) {
+                            if (in_tail) {
+                                const uint16_t *r = (const uint16_t *)(tailb + 32 * D) + lkey0 * D + d;
+                                v = make_uint4(r[0] | r[D] << 16, r[2 * D] | r[3 * D] << 16,
+                                               r[4 * D] | r[5 * D] << 16, r[6 * D] | r[7 * D] << 16);
+                            } else {
+                                const uint8_t *vq = vb + kBlock * D + ((lkey0 >> 2) * D + d) * 4;
+                                const uint2 w0 = i8_bf16x4(*(const uint32_t *)vq);
+                                const uint2 w1 = i8_bf16x4(*(const uint32_t *)(vq + 4 * D));
+                                v = make_uint4(w0.x, w0.y, w1.x, w1.y);
+                            }
                         } else {
                             v = ((const uint4 *)(vb + Lds::kTile + d * 32))[lg & 1];
                         }
@@ -1874,7 +2011,7 @@ bool attn_valu_supported(int dtype, int d, int g) {
 }
 
 bool prefill_mfma_supported(int dtype, int d, int g) {
-    return (((dtype == 0 || dtype == 1) && (d == 128 || d == 64)) || (dtype == 2 && d == 128)) && (g == 1 || g == 2 || g == 4 || g == 8);
+    return (((dtype == 0 || dtype == 1 || dtype == 3) && (d == 128 || d == 64)) || (dtype == 2 && d == 128)) && (g == 1 || g == 2 || g == 4 || g == 8);
 }
 
 hipError_t launch_plan_apply(const int32_t *src, int32_t *dst, int32_t n_words,
@@ -1980,20 +2117,21 @@ int prefill_rows_per_pass() { return kPfRowsPerPass; }
 // tile per wave) or the full kPfRowsPerPass
 bool prefill_pass_rows_valid(int rows) { return rows == kPfRowsPerPass || rows == kPfWaves * 16; }
 
-template <int D, bool F8, bool RF>
+template <int D, int FORM, bool RF>
 void launch_prefill_g(int G, dim3 grid, dim3 block, hipStream_t s, const PfArgs &pa) {
     switch (G) {
-        case 1: hipLaunchKernelGGL((k_prefill_mfma<D, 1, F8, RF>), grid, block, 0, s, pa); break;
-        case 2: hipLaunchKernelGGL((k_prefill_mfma<D, 2, F8, RF>), grid, block, 0, s, pa); break;
-        case 4: hipLaunchKernelGGL((k_prefill_mfma<D, 4, F8, RF>), grid, block, 0, s, pa); break;
-        default: hipLaunchKernelGGL((k_prefill_mfma<D, 8, F8, RF>), grid, block, 0, s, pa); break;
+        case 1: hipLaunchKernelGGL((k_prefill_mfma<D, 1, FORM, RF>), grid, block, 0, s, pa); break;
+        case 2: hipLaunchKernelGGL((k_prefill_mfma<D, 2, FORM, RF>), grid, block, 0, s, pa); break;
+        case 4: hipLaunchKernelGGL((k_prefill_mfma<D, 4, FORM, RF>), grid, block, 0, s, pa); break;
+        default: hipLaunchKernelGGL((k_prefill_mfma<D, 8, FORM, RF>), grid, block, 0, s, pa); break;
     }
 }
 
 hipError_t launch_prefill_mfma(int dtype, const AttnArgs &a, const int32_t *items, int32_t n_items,
-                               int32_t pass_rows, const uint8_t *zero_page, hipStream_t s) {
+                               int32_t pass_rows, const uint8_t *zero_page, const TailView &tails,
+                               hipStream_t s) {
     const int G = a.g.hq / a.g.hkv;
-    if (dtype == 0 || !prefill_mfma_supported(dtype, a.g.d, G) || n_items <= 0 || !zero_page || !items ||
+    if (dtype == 0 || (dtype == 3 && !tails.base) || !prefill_mfma_supported(dtype, a.g.d, G) || n_items <= 0 || !zero_page || !items ||
         !prefill_pass_rows_valid(pass_rows))
         return hipErrorInvalidValue;
     if (((uintptr_t)items & 31) != 0) return hipErrorInvalidValue;  // records are 32-byte aligned
@@ -2002,16 +2140,19 @@ hipError_t launch_prefill_mfma(int dtype, const AttnArgs &a, const int32_t *item
     if (a.n_split < 1 || a.n_split > kMaxSplit) return hipErrorInvalidValue;
     const int64_t wgs = (int64_t)n_items * a.g.hkv * a.n_split;
     if (wgs > INT32_MAX) return hipErrorInvalidValue;
-    PfArgs pa{a, items, zero_page, pass_rows};
+    PfArgs pa{a, items, zero_page, pass_rows, tails};
     dim3 grid((unsigned)wgs), block(64 * kPfWaves);
     auto launch = [&](auto rf) {
         constexpr bool RF = decltype(rf)::value;
         if (dtype == 2)
-            launch_prefill_g<128, true, RF>(G, grid, block, s, pa);
+            launch_prefill_g<128, kKvF8, RF>(G, grid, block, s, pa);
+        else if (dtype == 3)
+            a.g.d == 128 ? launch_prefill_g<128, kKvI8, RF>(G, grid, block, s, pa)
+                         : launch_prefill_g<64, kKvI8, RF>(G, grid, block, s, pa);
         else if (a.g.d == 128)
-            launch_prefill_g<128, false, RF>(G, grid, block, s, pa);
+            launch_prefill_g<128, kKvBf16, RF>(G, grid, block, s, pa);
         else
-            launch_prefill_g<64, false, RF>(G, grid, block, s, pa);
+            launch_prefill_g<64, kKvBf16, RF>(G, grid, block, s, pa);
     };
     if (rope_form(a.g))
         launch(std::true_type{});

@@ -1,5 +1,6 @@
 // gfx950 kernels that move whole pages of the pool: the fork of a session into
-// copies, and the move of every session's pages into another buffer.
+// copies, and the move of every session's pages into another buffer; of int8
+// pools also the sessions' tails.
 //
 // A page is one block of one layer (every KV head's tiles), `block_stride`
 // contiguous bytes of any cache type.  Bound by memory alone: a fork reads a
@@ -92,6 +93,13 @@ __global__ __launch_bounds__(kPageThreads) void k_move_table(MoveArgs a) {
         a.table[(int64_t)s.sid * a.row_len + page_lb(i, s.n_sink_pages, a.n_sink_blocks)] = s.base + i;
 }
 
+// workgroup (part, copy): an int8 pool's tails, every layer of one at a time
+__global__ __launch_bounds__(kPageThreads) void k_copy_tails(TailArgs a) {
+    const u32x4_t *src = (const u32x4_t *)(a.from + (int64_t)a.src[blockIdx.y] * a.stride);
+    u32x4_t *dst = (u32x4_t *)(a.to + (int64_t)a.dst[blockIdx.y] * a.stride);
+    copy_part(src, (int64_t)blockIdx.x * (kPart / 16), a.stride / 16, 1, [&](int) { return dst; });
+}
+
 uint32_t page_parts(int64_t block_stride) { return (uint32_t)((block_stride + kPart - 1) / kPart); }
 
 }  // namespace
@@ -114,6 +122,13 @@ hipError_t launch_move(const MoveArgs &a, int32_t n_layers, hipStream_t s) {
     if (a.n < 1 || a.n > kMoveSessions || x < 1 || x > INT32_MAX || n_layers > 65535 || a.block_stride % 16)
         return hipErrorInvalidValue;
     hipLaunchKernelGGL(k_move, dim3((unsigned)x, (unsigned)a.n, (unsigned)n_layers), dim3(kPageThreads), 0, s, a, parts);
+    return hipGetLastError();
+}
+
+hipError_t launch_copy_tails(const TailArgs &a, hipStream_t s) {
+    const int64_t x = (a.stride + kPart - 1) / kPart;
+    if (a.n < 1 || a.n > kTailCopies || a.stride < 1 || a.stride % 16 || x > INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(k_copy_tails, dim3((unsigned)x, (unsigned)a.n), dim3(kPageThreads), 0, s, a);
     return hipGetLastError();
 }
 

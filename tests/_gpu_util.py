@@ -12,8 +12,9 @@ from workload import session_rng, draw_qkv
 
 # io element type and output tolerance per pool dtype (the fp8 pool takes bf16
 # io; its oracle holds the E4M3 round trip of every stored row)
-TDT = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.bfloat16}
-TOL = {"f32": 1e-5, "bf16": 2e-2, "fp8": 2e-2}
+TDT = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.bfloat16, "int8": torch.bfloat16}
+TOL = {"f32": 1e-5, "bf16": 2e-2, "fp8": 2e-2, "int8": 6e-2}
+KV_QUANT = {"fp8": "fp8_e4m3", "int8": "int8_block"}
 
 
 def say(*a):
@@ -52,11 +53,12 @@ class Harness:
         self.dtype = dtype
         self.sids = [pool.session_open() for _ in range(n_sessions)]
         self.orc = [wa.OracleSession(hq, hkv, d, S, W, theta=theta, n_layers=n_layers,
-                                     kv_quant="fp8_e4m3" if dtype == "fp8" else None)
+                                     kv_quant=KV_QUANT.get(dtype))
                     for _ in range(n_sessions)]
         self.rng = [session_rng(1000 + seed, i) for i in range(n_sessions)]
         self.max_err = 0.0
         self.max_lse_err = 0.0
+        self.sq_err, self.n_err = 0.0, 0
 
     def _draw(self, i, n_tok):
         q, k, v = draw_qkv(self.rng[i], self.L, n_tok, self.hq, self.hkv, self.d)
@@ -79,10 +81,16 @@ class Harness:
         lerr = float(np.max(np.abs(f64(got_lse) - ref_lse))) if ref.size else 0.0
         self.max_err = max(self.max_err, err)
         self.max_lse_err = max(self.max_lse_err, lerr)
+        self.sq_err += float(np.sum((f64(got) - ref) ** 2))
+        self.n_err += ref.size
         tol = TOL[self.dtype]
         assert np.all(np.isfinite(f64(got))), f"{what}: non-finite output"
         assert err <= tol, f"{what}: max abs err {err:.3e} > {tol}"
         assert lerr <= max(tol, 1e-4), f"{what}: lse err {lerr:.3e}"
+
+    def rms_err(self):
+        """Root mean square of the output error over everything compared."""
+        return (self.sq_err / max(self.n_err, 1)) ** 0.5
 
     def frame(self, chunk_len, n_dec, n_split=0, check=True, use_frame_step=True, fused=False):
         n = len(self.sids)

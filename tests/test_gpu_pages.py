@@ -22,6 +22,16 @@ def _harness(dtype, hq, hkv, d, W=40, S=4, n=2, room=6, layers=2, cmax=9, spare=
     return Harness(pool, n_sessions=n, n_layers=layers, hq=hq, hkv=hkv, d=d, S=S, W=W, dtype=dtype, seed=3)
 
 
+def _code(call):
+    """The error code of a refused call.  (Kept exceptions would keep the pool, in
+    a cycle that a later test's collection frees, device synchronisation and all.)"""
+    try:
+        call()
+    except mtn.MtnError as e:
+        return e.code
+    return mtn.MTN_OK
+
+
 def _fork(h, i, copies, **kw):
     """Fork session i of the harness, oracle and generators with it; the copies'
     generators then draw other tokens."""
@@ -145,10 +155,9 @@ def test_refused_while_a_graph_is_captured():
     torch.cuda.synchronize()
     before, g = h.pool.stats(), torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
-        for call in (lambda: h.pool.session_fork(h.sids[0]), lambda: h.pool.resize(h.pool.cfg.n_blocks, kv)):
-            with pytest.raises(mtn.MtnError) as e:
-                call()
-            assert e.value.code == mtn.MTN_ERR_BAD_STATE
+        codes = [_code(lambda: h.pool.session_fork(h.sids[0])),
+                 _code(lambda: h.pool.resize(h.pool.cfg.n_blocks, kv))]
+    assert codes == [mtn.MTN_ERR_BAD_STATE] * 2
     assert h.pool.stats() == before
     _frames(h, rnd, 2)
 
@@ -159,7 +168,5 @@ def test_bad_buffers_are_refused():
     for kv, blocks in [(None, h.pool.cfg.n_blocks), (h.pool.kv, h.pool.cfg.n_blocks),
                        (torch.empty(n - 256, dtype=torch.uint8, device="cuda"), h.pool.cfg.n_blocks),
                        (torch.empty(n + 16, dtype=torch.uint8, device="cuda")[16:], h.pool.cfg.n_blocks)]:
-        with pytest.raises(mtn.MtnError) as e:
-            h.pool.resize(blocks, kv)
-        assert e.value.code == mtn.MTN_ERR_INVALID_ARG
+        assert _code(lambda: h.pool.resize(blocks, kv)) == mtn.MTN_ERR_INVALID_ARG
     _frames(h, random.Random(6), 2)
