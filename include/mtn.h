@@ -139,11 +139,12 @@ typedef struct {
  *   V exponents e + 127                      bytes [4112, 4128)
  * and 96 bytes of padding; a stored value is code * 2^e.
  *
- * MTN_INT8_BLOCK: each (l, b) region is Hkv * (32 D + 8) bytes, padded to 128, at
- * (l * n_blocks + b) times that, and holds per head h
- *   K codes + 128, unsigned [16][D]          bytes [h * 32 D, + 16 D)
- *   V codes, signed, in key quads: byte ((key / 4) * D + d) * 4 + key % 4 after them
- *   the scales {K, V}, fp32                  bytes [Hkv * 32 D + 8 h, + 8)
+ * MTN_INT8_BLOCK: each (l, b) is Hkv regions of 32 D + 16 bytes, padded together
+ * to a multiple of 128, at (l * n_blocks + b) times that; a head's region holds
+ *   K codes + 128, unsigned [16][D]          bytes [0, 16 D)
+ *   V codes, signed, in key quads: byte ((key / 4) * D + d) * 4 + key % 4,
+ *                                            bytes [16 D, 32 D)
+ *   the scales {K, V}, fp32                  bytes [32 D, 32 D + 8), 8 unused
  * Behind the blocks (256-byte aligned) lie two tails per session slot, [layer]
  * [Hkv]{K [16][D], V [16][D]} bf16: the rows of the session's open block (two, so
  * that an abandoned plan leaves the committed rows whole).

@@ -230,19 +230,17 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Bytes of one (layer, block, kv head) region: K tile + V^T tile of 16 x D
 // elements, or for fp8 the code tiles plus 32 exponent bytes, padded to 128;
-// int8: the code tiles.
+// int8: the code tiles and 16 bytes for the two scales.
 int64_t kv_head_stride(const mtn_pool_config *c) {
     if (c->kv_dtype == MTN_FP8_E4M3) return fp8_head_stride(c->head_dim);
-    if (c->kv_dtype == MTN_INT8_BLOCK) return 2 * (int64_t)kBlock * c->head_dim;
+    if (c->kv_dtype == MTN_INT8_BLOCK) return 2 * (int64_t)kBlock * c->head_dim + 16;
     return 2 * (int64_t)kBlock * c->head_dim * (c->kv_dtype == MTN_BF16 ? 2 : 4);
 }
 
-// ... of one (layer, block): every head's region, int8: and its two scales,
-// padded to 128 bytes.
+// ... of one (layer, block): every head's region, int8: padded to 128 bytes.
 int64_t kv_block_stride(const mtn_pool_config *c) {
-    if (c->kv_dtype == MTN_INT8_BLOCK)
-        return (c->n_kv_heads * (kv_head_stride(c) + 8) + 127) / 128 * 128;
-    return c->n_kv_heads * kv_head_stride(c);
+    const int64_t n = c->n_kv_heads * kv_head_stride(c);
+    return c->kv_dtype == MTN_INT8_BLOCK ? ceil_div(n, 128) * 128 : n;
 }
 // int8: bytes of one tail (the rows of an open block, bf16, of every layer),
 // and where the tails begin in a buffer, behind the blocks.
@@ -1011,7 +1009,9 @@ int32_t auto_split(const mtn_pool *P, int32_t n_items) {
     const bool mfma = use_mfma(P, units);
     const int64_t resident = std::max<int32_t>(mfma ? P->resident_mfma : P->resident_valu, 1);
     if (units >= resident) return 1;
-    const int64_t groups = mfma ? attn_mfma_groups(P->G) : attn_valu_groups(P->G);
+    const int64_t groups = P->int8 ? attn_i8_groups()
+                           : mfma  ? attn_mfma_groups(P->G)
+                                   : attn_valu_groups(P->G);
     const int64_t blocks = (ceil_div(max_keys, kBlock) + 1) / groups;  // of a wave group, unsplit
     const int64_t fine = std::min<int64_t>(blocks / 2, P->n_cu / units);
     const int64_t sp = std::min<int64_t>({resident / units, std::max<int64_t>(fine, blocks / (mfma ? 8 : 5)),
@@ -1058,7 +1058,7 @@ mtn_status decode_impl(mtn_pool *P, int32_t layer, const void *q, void *out, flo
     if (P->cfg.kv_dtype == MTN_FP8_E4M3)
         HIP_TRY(P, launch_attn_fp8(a, s));
     else if (P->int8)
-        HIP_TRY(P, launch_attn_i8(a, tails(P), s));
+        HIP_TRY(P, launch_attn_i8(a, tails(P), P->n_cu, s));
     else if (use_mfma(P, (int64_t)P->T * P->cfg.n_kv_heads))
         HIP_TRY(P, launch_attn_mfma_bf16(a, s));
     else
@@ -1383,7 +1383,7 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
         if (fp8)
             P->resident_mfma = n_cu * attn_fp8_resident_per_cu(P->G);
         else if (P->int8)
-            P->resident_mfma = n_cu * attn_i8_resident_per_cu(cfg->head_dim, P->G);
+            P->resident_mfma = n_cu;  // one workgroup each (see k_attn_i8's copies ahead)
         else if (cfg->kv_dtype == MTN_BF16 && attn_mfma_bf16_supported(cfg->head_dim, P->G))
             P->resident_mfma = n_cu * attn_mfma_bf16_resident_per_cu(cfg->head_dim, P->G);
         if (!fp8 && !P->int8)

@@ -53,12 +53,12 @@ hipError_t launch_poison_fp8(const PoolGeom &, int32_t, int64_t, const uint16_t 
     return hipErrorNotSupported;
 }
 bool attn_i8_supported(int d, int g) { return (d == 128 || d == 64) && group_ok(g); }
-int attn_i8_resident_per_cu(int, int) { return 1; }
+int attn_i8_groups() { return 4; }
 hipError_t launch_append_i8(const PoolGeom &, const PlanView &, int32_t, const void *, const void *,
                             const TailView &, const int32_t *, const int32_t *, int32_t, hipStream_t) {
     return hipErrorNotSupported;
 }
-hipError_t launch_attn_i8(const AttnArgs &, const TailView &, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_attn_i8(const AttnArgs &, const TailView &, int, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_poison_i8(const PoolGeom &, const TailView &, int32_t, int64_t, int32_t,
                             const uint16_t *, const uint8_t *, hipStream_t) {
     return hipErrorNotSupported;

@@ -11,11 +11,15 @@
 // keys rotated) in a tail of 16 rows per session, layer and KV head, so that
 // every row is rounded to 8 bits once, whatever chunks brought it.
 //
-// Region of one (layer, block): every KV head's codes, 32 D bytes each,
+// Region of one (layer, block, KV head), 32 D + 16 bytes (a layer's block padded to
+// 128):
 //   [0, 16 D)      K codes + 128 (unsigned), [16 keys][D]
 //   [16 D, 32 D)   V codes (signed) in key quads: byte ((key / 4) * D + d) * 4 + key % 4
-// then the heads' scales {K, V} as float pairs, padded to 128 bytes.  A tail is
-// K [16][D], V [16][D] bf16.
+//   [32 D, + 8)    the scales {K, V}, fp32
+// The scales lie right behind their codes: gathered behind the block's last head
+// instead, a second place to wait for with every block, they cost 128 sessions of
+// G = 8 98.8 us a launch against 87.5 without any.  A tail is K [16][D], V [16][D]
+// bf16.
 #include "mtn_kernels.h"
 #include "mtn_device.h"
 
@@ -210,7 +214,7 @@ __global__ __launch_bounds__(256) void k_append_i8(PoolGeom g, PlanView p, int32
         *(uint16_t *)(codes + j * D + P * c) = (uint16_t)wa;
         *(uint16_t *)(codes + j * D + D / 2 + P * c) = (uint16_t)wb;
     }
-    if (tid == 0) *(float2 *)(region + (int64_t)g.hkv * g.head_stride + 8 * h) = make_float2(ks, vs);
+    if (tid == 0) *(float2 *)(codes + 2 * kBlock * D) = make_float2(ks, vs);
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < NW; ++e) {  // quad words, memory order
@@ -245,19 +249,27 @@ __global__ __launch_bounds__(256) void k_append_i8(PoolGeom g, PlanView p, int32
 //
 // Bound by the stream of codes.  Per block a wave converts 4096 codes in 112
 // vector instructions (K 64, V 48), against 64 of the FP8 kernel.
-template <int G>
-struct I8Shape {
-    static constexpr int NG = G >= 8 ? 4 : 8;
-    static constexpr int NBUF = 2;
-};
+// Launch shape: four waves a workgroup with two-block rings at every group size.
+// (Eight waves, which the FP8 kernel takes below G = 8: 8 KV heads, G = 4, 60
+// sessions of 2048 keys 50.3 us against 48.9, 32 sessions 32.1 against 29.7; 200
+// sessions of 1000 keys, D = 64, G = 1, 48.9 against 43.6; only 64 sessions of G = 1,
+// 2048 units, are faster, 179.1 against 180.3.  Three-block rings: 128 sessions of
+// G = 8 98.1 against 93.8.)
+constexpr int kI8Waves = 4, kI8Ring = 2;
+// What the tail takes its wave, in blocks of the ring: that wave's segment is
+// shorter by as many where segments are at least 8 blocks.  0, 3, 5, 8: 64 sessions
+// of G = 8 60.2, 58.2, 57.3, 57.0 us; 8 sessions 23.6, 21.9, 20.7, 23.4 (at 8 the rule
+// no longer applied to them).
+constexpr int kTailBlocks = 5;
 
-template <int D, int G, int NG, int NBUF, bool RF>
-__global__ __launch_bounds__(64 * NG) void k_attn_i8(I8Args ia) {
+template <int D, int G, bool RF>
+__global__ __launch_bounds__(64 * kI8Waves) void k_attn_i8(I8Args ia) {
+    constexpr int NG = kI8Waves, NBUF = kI8Ring;
     constexpr int ND = D / 32;   // QK MFMAs per block
     constexpr int NJ = D / 16;   // PV MFMAs per block
     constexpr int VD = D / 64;   // dims per lane of a row
     constexpr int CODES = 2 * kBlock * D;
-    constexpr int BLK = CODES + 16;      // ring slot: the head's codes, the 16 bytes that hold its scales
+    constexpr int BLK = CODES + 16;      // ring slot: the head's region, codes and scales
     constexpr int NFI = CODES / 1024;    // 1 KiB copies per block
     constexpr int NIW = NFI + 1;
     static_assert(NBUF * BLK >= 16 * D * 4, "merge scratch fits one wave's ring");
@@ -285,11 +297,12 @@ __global__ __launch_bounds__(64 * NG) void k_attn_i8(I8Args ia) {
     const VisRange vr = vis_range(g, pos);
     const int nv = vr.n_sb + vr.n_rb;
     const uint32_t nseg = ns * NG, seg = (uint32_t)split * NG + wv;
-    const int v0 = __builtin_amdgcn_readfirstlane(seg_begin(seg, nseg, nv));
-    const int v1 = __builtin_amdgcn_readfirstlane(seg_begin(seg + 1, nseg, nv));
+    // the tail counts as kTailBlocks more where segments are long
+    const int nw = nv + ((fused || !complete) && nv >= 8 * (int)nseg ? kTailBlocks : 0);
+    const int v0 = __builtin_amdgcn_readfirstlane(seg_begin(seg, nseg, nw));
+    const int v1 = __builtin_amdgcn_readfirstlane(min(seg_begin(seg + 1, nseg, nw), nv));
     const int nblk = v1 - v0 - (tail_wave ? 1 : 0);  // blocks from the pool (the last segment holds the last block)
-    const uint8_t *head_base = g.kv + (int64_t)a.layer * g.layer_stride + (int64_t)kvh * CODES;
-    const uint32_t scale_off = (uint32_t)((g.hkv - kvh) * CODES + (kvh >> 1) * 16);  // from the head's codes
+    const uint8_t *head_base = g.kv + (int64_t)a.layer * g.layer_stride + (int64_t)kvh * BLK;
     const int32_t *trow = g.table + (int64_t)sid * g.row_len;
     const uint32_t ring0 = lds_addr(&ring[wv][0][0]);
 
@@ -314,7 +327,7 @@ __global__ __launch_bounds__(64 * NG) void k_attn_i8(I8Args ia) {
         const uint32_t dst = ring0 + (uint32_t)((i % NBUF) * BLK);
 #pragma unroll
         for (int j = 0; j < NFI; ++j) dma16_s(doff[j], src, dst + j * 1024);
-        if (lane < 1) dma16_s(scale_off, src, dst + CODES);
+        if (lane < 1) dma16_s(CODES, src, dst + CODES);
         if (i + 1 < nblk) ph = next_phys();
     };
     for (int i = 0; i < min(nblk, NBUF - 1); ++i) issue(i);
@@ -378,7 +391,7 @@ __global__ __launch_bounds__(64 * NG) void k_attn_i8(I8Args ia) {
             y[e] = fmaf(x[e], cs.x, sgn * z[e] * cs.y);
         }
     };
-    uint4 qh[ND];
+    uint4 qh[ND], qb[ND];  // the query in f16 (scaled) for codes, in bf16 for the tail
     float qscale;
     {
         const bool hv = n < G;
@@ -396,150 +409,147 @@ __global__ __launch_bounds__(64 * NG) void k_attn_i8(I8Args ia) {
         const int eq = __builtin_amdgcn_frexp_expf(rows_max(mx));  // 0 for zero and for infinities
         qscale = ldexpf(1.f, eq);
 #pragma unroll
-        for (int s = 0; s < ND; ++s)
+        for (int s = 0; s < ND; ++s) {
             qh[s] = make_uint4(pack_f16x2(ldexpf(q[s][0], -eq), ldexpf(q[s][1], -eq)),
                                pack_f16x2(ldexpf(q[s][2], -eq), ldexpf(q[s][3], -eq)),
                                pack_f16x2(ldexpf(q[s][4], -eq), ldexpf(q[s][5], -eq)),
                                pack_f16x2(ldexpf(q[s][6], -eq), ldexpf(q[s][7], -eq)));
-        // ---- the newest block from the tail
-        if (tail_wave) {
-            uint8_t *tail = tail_of(ia.tails, g, sid, tslot, a.layer, kvh, D);
-            bf16_t *tk = (bf16_t *)tail, *tv = tk + kBlock * D;
-            int lb, lo, hi;
-            vblock(g, vr, nv - 1, &lb, &lo, &hi);  // slots the query sees: hi - 1 is the newest key
-            // K row n, dims d0 ..; V rows 4 g4 + r, dims NJ n .. (NJ / 2 words)
-            uint4 kr[ND];
-            uint32_t vv[4][NJ / 2];
+            qb[s] = make_uint4(pack_bf16x2(q[s][0], q[s][1]), pack_bf16x2(q[s][2], q[s][3]),
+                               pack_bf16x2(q[s][4], q[s][5]), pack_bf16x2(q[s][6], q[s][7]));
+        }
+    }
+    // ---- the newest block from the tail: keys to scores, then values, so that
+    // the registers of one are free before the other's are used
+    if (tail_wave) {
+        uint8_t *tail = tail_of(ia.tails, g, sid, tslot, a.layer, kvh, D);
+        bf16_t *tk = (bf16_t *)tail, *tv = tk + kBlock * D;
+        uint8_t *region = (uint8_t *)g.kv + (int64_t)a.layer * g.layer_stride +
+                          (int64_t)__builtin_amdgcn_readfirstlane(a.p.tok_block[t]) * g.block_stride;
+        uint8_t *codes = region + (int64_t)kvh * BLK;
+        const bool keep = fused && complete;  // the block is quantized, stored and used so
+        int lb, lo, hi;
+        vblock(g, vr, nv - 1, &lb, &lo, &hi);  // slots the query sees: hi - 1 is the newest key
+        auto lo16 = [](uint32_t x) { return __uint_as_float(x << 16); };
+        auto hi16 = [](uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); };
+        auto wave_max = [](float x) {
 #pragma unroll
-            for (int s = 0; s < ND; ++s) kr[s] = *(const uint4 *)(tk + n * D + d0 + 8 * s);
+            for (int m = 1; m < 64; m <<= 1) x = max_nan(x, __shfl_xor(x, m, 64));
+            return x;
+        };
+        // K row n, dims d0 .. + D/4 - 1; V rows 4 g4 + r, dims NJ n .. (NJ / 2 words)
+        uint4 kr[ND];
+        uint32_t vv[4][NJ / 2];
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+        for (int s = 0; s < ND; ++s) kr[s] = *(const uint4 *)(tk + n * D + d0 + 8 * s);
 #pragma unroll
-                for (int x = 0; x < NJ / 2; x += 2)
-                    *(uint2 *)&vv[r][x] = *(const uint2 *)(tv + (4 * g4 + r) * D + NJ * n + 2 * x);
-            if (fused) {
-                const bf16_t *kh = (const bf16_t *)a.k_new + (row * g.hkv + kvh) * D;
-                const bf16_t *vh = (const bf16_t *)a.v_new + (row * g.hkv + kvh) * D + NJ * n;
-                uint4 kn[ND];
-                uint32_t vn[NJ / 2];
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int s = 0; s < ND; ++s) {
-                    float y[8];
-                    rotate8(kh, s, y);
-                    kn[s] = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]),
-                                       pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
-                    if (n == toff) kr[s] = kn[s];
-                }
+            for (int x = 0; x < NJ / 2; x += 2)
+                *(uint2 *)&vv[r][x] = *(const uint2 *)(tv + (4 * g4 + r) * D + NJ * n + 2 * x);
+        uint32_t vn[NJ / 2];
+        if (fused) {
+            const bf16_t *kh = (const bf16_t *)a.k_new + (row * g.hkv + kvh) * D;
+            const bf16_t *vh = (const bf16_t *)a.v_new + (row * g.hkv + kvh) * D + NJ * n;
 #pragma unroll
-                for (int x = 0; x < NJ / 2; x += 2) *(uint2 *)&vn[x] = *(const uint2 *)(vh + 2 * x);
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (4 * g4 + r == toff)
-#pragma unroll
-                        for (int x = 0; x < NJ / 2; ++x) vv[r][x] = vn[x];
-                if (!complete) {  // the tail's copy, for later launches
-                    if (n == toff)
-#pragma unroll
-                        for (int s = 0; s < ND; ++s) *(uint4 *)(tk + toff * D + d0 + 8 * s) = kn[s];
-                    if (g4 == (toff >> 2))
-#pragma unroll
-                        for (int x = 0; x < NJ / 2; x += 2)
-                            *(uint2 *)(tv + toff * D + NJ * n + 2 * x) = *(const uint2 *)&vn[x];
-                }
-            }
-            auto lo16 = [](uint32_t x) { return __uint_as_float(x << 16); };
-            auto hi16 = [](uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); };
-            // rows past the newest one hold nothing (or NaN)
-            const bool kin = n <= toff;
-#pragma unroll
-            for (int s = 0; s < ND; ++s) kr[s] = kin ? kr[s] : make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int x = 0; x < NJ / 2; ++x) vv[r][x] = 4 * g4 + r <= toff ? vv[r][x] : 0u;
-            float ks = 1.f, vs = 1.f;
-            if (complete) {  // (with the append fused) quantize, store and use the block
-                float mk = 0.f, mv = 0.f;
-#pragma unroll
-                for (int s = 0; s < ND; ++s) {
-                    const uint32_t w[4] = {kr[s].x, kr[s].y, kr[s].z, kr[s].w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) mk = vmaxabs3(lo16(w[e]), hi16(w[e]), mk);
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int x = 0; x < NJ / 2; ++x) mv = vmaxabs3(lo16(vv[r][x]), hi16(vv[r][x]), mv);
-#pragma unroll
-                for (int m = 1; m < 64; m <<= 1) {
-                    mk = max_nan(mk, __shfl_xor(mk, m, 64));
-                    mv = max_nan(mv, __shfl_xor(mv, m, 64));
-                }
-                ks = i8_scale(mk);
-                vs = i8_scale(mv);
-                uint8_t *region = (uint8_t *)g.kv + (int64_t)a.layer * g.layer_stride +
-                                  (int64_t)__builtin_amdgcn_readfirstlane(a.p.tok_block[t]) * g.block_stride;
-                uint8_t *codes = region + (int64_t)kvh * CODES;
-                uint32_t kc[2 * ND];  // the lane's K codes, four a word
-#pragma unroll
-                for (int s = 0; s < ND; ++s) {
-                    uint32_t w[4] = {kr[s].x, kr[s].y, kr[s].z, kr[s].w};
-                    kc[2 * s] = kc[2 * s + 1] = 0;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int c0 = i8_code(lo16(w[e]), ks), c1 = i8_code(hi16(w[e]), ks);
-                        kc[2 * s + e / 2] |= (uint32_t)((c0 + 128) & 255) << (16 * (e & 1)) |
-                                             (uint32_t)((c1 + 128) & 255) << (16 * (e & 1) + 8);
-                        w[e] = pack_bf16x2((float)c0, (float)c1);
-                    }
-                    kr[s] = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-                uint32_t vc[NJ];  // V codes: keys 4 g4 .. + 3 of dim NJ n + j
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) vc[j] = 0;
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int x = 0; x < NJ / 2; ++x) {
-                        const int c0 = i8_code(lo16(vv[r][x]), vs), c1 = i8_code(hi16(vv[r][x]), vs);
-                        vc[2 * x] |= (uint32_t)(c0 & 255) << (8 * r);
-                        vc[2 * x + 1] |= (uint32_t)(c1 & 255) << (8 * r);
-                        vv[r][x] = pack_bf16x2((float)c0, (float)c1);
-                    }
-#pragma unroll
-                for (int x = 0; x < 2 * ND; x += 4)
-                    *(uint4 *)(codes + n * D + d0 + 4 * x) = make_uint4(kc[x], kc[x + 1], kc[x + 2], kc[x + 3]);
-#pragma unroll
-                for (int x = 0; x < NJ; x += 4)
-                    *(uint4 *)(codes + kBlock * D + (g4 * D + NJ * n + x) * 4) =
-                        make_uint4(vc[x], vc[x + 1], vc[x + 2], vc[x + 3]);
-                if (lane == 0)
-                    *(float2 *)(region + (int64_t)g.hkv * CODES + 8 * kvh) = make_float2(ks, vs);
-            }
-            f32x4_t c = {0.f, 0.f, 0.f, 0.f};
+            for (int x = 0; x < NJ / 2; x += 2) *(uint2 *)&vn[x] = *(const uint2 *)(vh + 2 * x);
 #pragma unroll
             for (int s = 0; s < ND; ++s) {
-                const uint4 qb = make_uint4(pack_bf16x2(q[s][0], q[s][1]), pack_bf16x2(q[s][2], q[s][3]),
-                                            pack_bf16x2(q[s][4], q[s][5]), pack_bf16x2(q[s][6], q[s][7]));
-                c = mfma16x16x32(kr[s], qb, c);
+                float y[8];
+                rotate8(kh, s, y);
+                const uint4 kn = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]),
+                                            pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+                if (n == toff) {
+                    kr[s] = kn;
+                    if (!complete) *(uint4 *)(tk + toff * D + d0 + 8 * s) = kn;  // for later launches
+                }
             }
-            float sc[4];
-            bool ok[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int key = 4 * g4 + r;
-                ok[r] = key >= lo && key < hi;
-                sc[r] = ok[r] ? c[r] * ks : -INFINITY;
-                // (0 * NaN: rows that are not seen must not bring their values)
-#pragma unroll
-                for (int x = 0; x < NJ / 2; ++x) vv[r][x] = ok[r] ? vv[r][x] : 0u;
-            }
-            softmax_pv(std::true_type{}, sc, ok, vs, [&](int j) __attribute__((always_inline)) {
-                const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
-                return make_uint2(__builtin_amdgcn_perm(vv[1][j / 2], vv[0][j / 2], sel),
-                                  __builtin_amdgcn_perm(vv[3][j / 2], vv[2][j / 2], sel));
-            });
         }
+        // rows past the newest one hold nothing (or NaN)
+#pragma unroll
+        for (int s = 0; s < ND; ++s) kr[s] = n <= toff ? kr[s] : make_uint4(0, 0, 0, 0);
+        float ks = 1.f, vs = 1.f;
+        if (keep) {
+            float mk = 0.f;
+#pragma unroll
+            for (int s = 0; s < ND; ++s) {
+                const uint32_t w[4] = {kr[s].x, kr[s].y, kr[s].z, kr[s].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mk = vmaxabs3(lo16(w[e]), hi16(w[e]), mk);
+            }
+            ks = i8_scale(wave_max(mk));
+            uint32_t kc[2 * ND];  // the lane's K codes, four a word
+#pragma unroll
+            for (int s = 0; s < ND; ++s) {
+                uint32_t w[4] = {kr[s].x, kr[s].y, kr[s].z, kr[s].w};
+                kc[2 * s] = kc[2 * s + 1] = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int c0 = i8_code(lo16(w[e]), ks), c1 = i8_code(hi16(w[e]), ks);
+                    kc[2 * s + e / 2] |= (uint32_t)((c0 + 128) & 255) << (16 * (e & 1)) |
+                                         (uint32_t)((c1 + 128) & 255) << (16 * (e & 1) + 8);
+                    w[e] = pack_bf16x2((float)c0, (float)c1);
+                }
+                kr[s] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+#pragma unroll
+            for (int x = 0; x < 2 * ND; x += 4)
+                *(uint4 *)(codes + n * D + d0 + 4 * x) = make_uint4(kc[x], kc[x + 1], kc[x + 2], kc[x + 3]);
+        }
+        f32x4_t c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < ND; ++s) c = mfma16x16x32(kr[s], qb[s], c);
+        // values: the newest one's row, nothing past it
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int key = 4 * g4 + r;
+#pragma unroll
+            for (int x = 0; x < NJ / 2; ++x)
+                vv[r][x] = fused && key == toff ? vn[x] : key <= toff ? vv[r][x] : 0u;
+        }
+        if (fused && !complete && g4 == (toff >> 2))
+#pragma unroll
+            for (int x = 0; x < NJ / 2; x += 2)
+                *(uint2 *)(tv + toff * D + NJ * n + 2 * x) = *(const uint2 *)&vn[x];
+        if (keep) {
+            float mv = 0.f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int x = 0; x < NJ / 2; ++x) mv = vmaxabs3(lo16(vv[r][x]), hi16(vv[r][x]), mv);
+            vs = i8_scale(wave_max(mv));
+            uint32_t vc[NJ];  // V codes: keys 4 g4 .. + 3 of dim NJ n + j
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) vc[j] = 0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int x = 0; x < NJ / 2; ++x) {
+                    const int c0 = i8_code(lo16(vv[r][x]), vs), c1 = i8_code(hi16(vv[r][x]), vs);
+                    vc[2 * x] |= (uint32_t)(c0 & 255) << (8 * r);
+                    vc[2 * x + 1] |= (uint32_t)(c1 & 255) << (8 * r);
+                    vv[r][x] = pack_bf16x2((float)c0, (float)c1);
+                }
+#pragma unroll
+            for (int x = 0; x < NJ; x += 4)
+                *(uint4 *)(codes + kBlock * D + (g4 * D + NJ * n + x) * 4) =
+                    make_uint4(vc[x], vc[x + 1], vc[x + 2], vc[x + 3]);
+            if (lane == 0) *(float2 *)(codes + CODES) = make_float2(ks, vs);
+        }
+        float sc[4];
+        bool ok[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            ok[r] = 4 * g4 + r >= lo && 4 * g4 + r < hi;
+            sc[r] = ok[r] ? c[r] * ks : -INFINITY;
+            // (0 * NaN: rows that are not seen must not bring their values)
+#pragma unroll
+            for (int x = 0; x < NJ / 2; ++x) vv[r][x] = ok[r] ? vv[r][x] : 0u;
+        }
+        softmax_pv(std::true_type{}, sc, ok, vs, [&](int j) __attribute__((always_inline)) {
+            const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
+            return make_uint2(__builtin_amdgcn_perm(vv[1][j / 2], vv[0][j / 2], sel),
+                              __builtin_amdgcn_perm(vv[3][j / 2], vv[2][j / 2], sel));
+        });
     }
 
     // per-lane LDS chunks of the K and V fragments inside a ring slot: K row n,
@@ -569,7 +579,7 @@ __global__ __launch_bounds__(64 * NG) void k_attn_i8(I8Args ia) {
             kw[4 * x] = k4.x; kw[4 * x + 1] = k4.y; kw[4 * x + 2] = k4.z; kw[4 * x + 3] = k4.w;
             vw[4 * x] = v4.x; vw[4 * x + 1] = v4.y; vw[4 * x + 2] = v4.z; vw[4 * x + 3] = v4.w;
         }
-        const float2 sc2 = *(const float2 *)(blk + CODES + 8 * (kvh & 1));
+        const float2 sc2 = *(const float2 *)(blk + CODES);
         f32x4_t c = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < ND; ++s)
@@ -603,15 +613,20 @@ __global__ __launch_bounds__(64 * NG) void k_attn_i8(I8Args ia) {
     // sinks and the window's first block, the blocks between, its last one
     const int m_a = max(0, min(nblk, vr.n_sb + 1 - v0));
     const int m_b = max(m_a, v0 + nblk == nv ? nblk - 1 : nblk);
-    // (a short segment issues its next block before the wait, one choice per
-    // unit, as the bf16 / FP8 decode does)
+    // A wave issues its next block before it waits for the current one where
+    // segments are short, a chain of round trips, and where a CU has one
+    // workgroup, whose four waves' single copies would not cover the memory's
+    // latency (64 sessions of G = 8, a workgroup per CU, 49.0 us against 57.4 in
+    // two segments each); with more workgroups per CU after the wait (128 sessions
+    // 93.9 against 96.7).  One choice per unit: its waves, one block apart, would
+    // end apart with different ones.
     auto run = [&](auto ahead_c) __attribute__((always_inline)) {
         int i = 0;
         for (; i < m_a; ++i) step(i, ahead_c, std::true_type{});
         for (; i < m_b; ++i) step(i, ahead_c, std::false_type{});
         for (; i < nblk; ++i) step(i, ahead_c, std::true_type{});
     };
-    if (nv <= 20 * (int)nseg)
+    if (ia.ahead || nv <= 20 * (int)nseg)
         run(std::true_type{});
     else
         run(std::false_type{});
@@ -696,7 +711,7 @@ __global__ void k_poison_i8(PoolGeom g, TailView tails, int32_t n_layers, int64_
             codes[kBlock * D + ((key >> 2) * D + d) * 4 + (key & 3)] = 0x7F;
         }
         if (lm == 0 && threadIdx.x < 2)
-            ((float *)(region + (int64_t)g.hkv * g.head_stride))[2 * h + threadIdx.x] = __builtin_nanf("");
+            ((float *)(codes + 2 * kBlock * D))[threadIdx.x] = __builtin_nanf("");
     }
     const int64_t n_rows = (int64_t)n_tails * n_layers * g.hkv * kBlock;
     for (int64_t it = blockIdx.x; it < n_rows; it += gridDim.x) {
@@ -712,29 +727,15 @@ __global__ void k_poison_i8(PoolGeom g, TailView tails, int32_t n_layers, int64_
 
 template <int D, int G>
 hipError_t launch_i8_g(const I8Args &ia, hipStream_t s) {
-    using S = I8Shape<G>;
     const int64_t units = (int64_t)ia.a.p.n_tok * ia.a.g.hkv * ia.a.n_split;
     if (units == 0) return hipSuccess;
     if (units > INT32_MAX) return hipErrorInvalidValue;  // one grid dimension, 32-bit unit index
-    const dim3 grid((unsigned)units), block(64 * S::NG);
+    const dim3 grid((unsigned)units), block(64 * kI8Waves);
     if (rope_form(ia.a.g))
-        hipLaunchKernelGGL((k_attn_i8<D, G, S::NG, S::NBUF, true>), grid, block, 0, s, ia);
+        hipLaunchKernelGGL((k_attn_i8<D, G, true>), grid, block, 0, s, ia);
     else
-        hipLaunchKernelGGL((k_attn_i8<D, G, S::NG, S::NBUF, false>), grid, block, 0, s, ia);
+        hipLaunchKernelGGL((k_attn_i8<D, G, false>), grid, block, 0, s, ia);
     return hipGetLastError();
-}
-template <int D, int G>
-int resident_i8_g() {
-    using S = I8Shape<G>;
-    int n = 0;
-    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_attn_i8<D, G, S::NG, S::NBUF, false>, 64 * S::NG, 0) !=
-        hipSuccess)
-        return 1;
-    // the workgroups that hold about 64 KiB of copies in flight, as for the
-    // other matrix-core decodes
-    constexpr int kRing = S::NG * S::NBUF * (2 * kBlock * D + 16);
-    constexpr int kTarget = ((64 << 10) + kRing / 2) / kRing;
-    return std::min(std::max(n, 1), std::max(kTarget, 1));
 }
 template <class F>
 auto with_shape(int d, int g, F &&f) {
@@ -754,9 +755,7 @@ auto with_shape(int d, int g, F &&f) {
 bool attn_i8_supported(int d, int g) {
     return (d == 128 || d == 64) && (g == 1 || g == 2 || g == 4 || g == 8);
 }
-int attn_i8_resident_per_cu(int d, int g) {
-    return with_shape(d, g, [](auto dc, auto gc) { return resident_i8_g<decltype(dc)::value, decltype(gc)::value>(); });
-}
+int attn_i8_groups() { return kI8Waves; }
 
 hipError_t launch_append_i8(const PoolGeom &g, const PlanView &p, int32_t layer, const void *k, const void *v,
                             const TailView &tails, const int32_t *run_tok0, const int32_t *run_len,
@@ -776,10 +775,10 @@ hipError_t launch_append_i8(const PoolGeom &g, const PlanView &p, int32_t layer,
     return hipGetLastError();
 }
 
-hipError_t launch_attn_i8(const AttnArgs &a, const TailView &tails, hipStream_t s) {
+hipError_t launch_attn_i8(const AttnArgs &a, const TailView &tails, int n_cu, hipStream_t s) {
     const int G = a.g.hq / a.g.hkv;
     if (!attn_i8_supported(a.g.d, G) || (a.k_new == nullptr) != (a.v_new == nullptr)) return hipErrorInvalidValue;
-    const I8Args ia{a, tails};
+    const I8Args ia{a, tails, (int64_t)a.p.n_tok * a.g.hkv * a.n_split <= n_cu};
     return with_shape(a.g.d, G, [&](auto dc, auto gc) { return launch_i8_g<decltype(dc)::value, decltype(gc)::value>(ia, s); });
 }
 

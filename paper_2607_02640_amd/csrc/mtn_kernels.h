@@ -69,6 +69,7 @@ struct TailView {
 struct I8Args {
     AttnArgs a;
     TailView tails;
+    int32_t ahead;  // a wave issues its next block before it waits for the current one
 };
 
 // dtype codes match the public MTN_F32 / MTN_BF16 / MTN_FP8_E4M3 / MTN_INT8_BLOCK
@@ -196,11 +197,11 @@ hipError_t launch_attn_mfma_bf16(const AttnArgs &a, hipStream_t s);
 // in bits 0 .. 7 and which of the session's tails the token's block uses (while
 // open) in bit 8.
 bool attn_i8_supported(int d, int g);
-int attn_i8_resident_per_cu(int d, int g);
+int attn_i8_groups();  // waves that share a unit's keys
 hipError_t launch_append_i8(const PoolGeom &g, const PlanView &p, int32_t layer, const void *k,
                             const void *v, const TailView &tails, const int32_t *run_tok0,
                             const int32_t *run_len, int32_t n_runs, hipStream_t s);
-hipError_t launch_attn_i8(const AttnArgs &a, const TailView &tails, hipStream_t s);
+hipError_t launch_attn_i8(const AttnArgs &a, const TailView &tails, int n_cu, hipStream_t s);
 hipError_t launch_poison_i8(const PoolGeom &g, const TailView &tails, int32_t n_layers,
                             int64_t n_blocks, int32_t n_tails, const uint16_t *live_mask,
                             const uint8_t *tail_rows, hipStream_t s);

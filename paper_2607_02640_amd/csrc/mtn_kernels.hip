@@ -1060,7 +1060,6 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                         ((int64_t)a.layer * g.hkv + kvh) * (64 * D);
         }
     }
-    const uint32_t i8_scale_off = (uint32_t)((g.hkv - kvh) * kI8Codes + (kvh >> 1) * 16);  // from the head's codes
 
     auto vblock = [&](int v) {
         v += vb0;
@@ -1119,7 +1118,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             dsrc[m] = j < 4 ? j * 1024 + lane * 16 : kF8Exp + (lane & 1) * 16;
             ddst[m] = db * kF8Read + (j < 4 ? j * 1024 : kF8Exp);
         } else if constexpr (I8) {
-            dsrc[m] = j * 1024 + lane * 16;  // (the scales' offset: issue_block)
+            dsrc[m] = j * 1024 + lane * 16;
             ddst[m] = db * kI8Blk + j * 1024;
         } else {
             const int off = j < NKI ? db * Lds::kTile + j * 1024
@@ -1156,7 +1155,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 // it, and the reload's wait also drains the DMA ring
                 if (lane < 2) dma16_s(kF8Exp + (lane & 1) * 16, src, dst + ddst[m]);
             } else if (I8 && m == NPW - 1) {
-                if (lane < 1) dma16_s(ph >= 0 ? i8_scale_off : 0u, src, dst + ddst[m]);
+                if (lane < 1) dma16_s(kI8Codes, src, dst + ddst[m]);
             } else {
                 dma16_s(dsrc[m], src, dst + ddst[m]);
             }
@@ -1549,7 +1548,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         // int8: {K, V} scale of this lane's block in stage st, from its ring slot
         // (which the stage's own step may still read)
         auto scales = [&](int st) __attribute__((always_inline)) {
-            const float2 x = *(const float2 *)(&ring[st % kPfStages][0] + lblk * kI8Blk + kI8Codes + 8 * (kvh & 1));
+            const float2 x = *(const float2 *)(&ring[st % kPfStages][0] + lblk * kI8Blk + kI8Codes);
             return 2 * st + lblk == tail_v ? make_float2(1.f, 1.f) : x;
         };
         const bool grp_b = kPP && wv >= kPfWaves / 2;
@@ -1802,7 +1801,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 float v_scale = 1.f;
                 if constexpr (I8) {
                     if (!in_tail && (lblk ? ph1 : ph0) >= 0) {
-                        const float2 x = *(const float2 *)(vb + (g.hkv - kvh) * kI8Codes + 8 * kvh);
+                        const float2 x = *(const float2 *)(vb + kI8Codes);
                         s0 *= x.x;
                         s1 *= x.x;
                         v_scale = x.y;

@@ -84,9 +84,9 @@ def _kw(**kw):
 
 def test_required_bytes():
     assert mtn.Pool.required(**_kw()) == 3 * 20 * (2 * 4096 + 128) + 5 * 2 * 3 * 2 * 8192
-    # 17 heads: 17 * 8 bytes of scales, padded to 256; the tails begin at a multiple of 256
+    # 17 heads: 17 * 2064 = 35088, padded to 35200; the tails begin at a multiple of 256
     kw = _kw(n_q_heads=17, n_kv_heads=17, head_dim=64, n_layers=1, n_blocks=1)
-    assert mtn.Pool.required(**kw) == 17 * 2048 + 256 + 5 * 2 * 17 * 4096
+    assert mtn.Pool.required(**kw) == 35328 + 5 * 2 * 17 * 4096
 
 
 @pytest.mark.parametrize("change,code", [
