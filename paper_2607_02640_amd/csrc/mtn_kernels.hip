@@ -971,6 +971,7 @@ __device__ __forceinline__ void i8_stage_to_bf16(const uint8_t *src, int blk, ui
 // What the pool holds: bf16 rows, E4M3 codes, or int8 codes.
 enum KvForm { kKvBf16, kKvF8, kKvI8 };
 
+// I8: the pool holds int8 codes; a stage lands as two regions, codes and scales.
 // F8: the pool holds E4M3 codes.  Each stage then lands as two kF8Read-byte
 // regions (per block four 1 KiB DMA instructions plus the 32 exponent
 // bytes), and every stage is converted into one of two bf16 stage buffers (a
@@ -987,7 +988,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
     static_assert(kPfStages >= 3 && kPfStages <= 8, "ring depth (the DMA waits count at most 63)");
     static_assert(kPfEarly >= 1 && kPfEarly <= kPfStages - 1, "early stages are ring prologue stages");
     __shared__ __attribute__((aligned(16))) uint8_t ring[kPfStages][SB];
-    __shared__ __attribute__((aligned(16))) uint8_t bfs[Q8 ? 2 : 1][Q8 ? Lds::kStage : 16];
+    __shared__ __attribute__((aligned(16))) uint8_t bfs[I8 ? 4 : F8 ? 2 : 1][Q8 ? Lds::kStage : 16];
     __shared__ __attribute__((aligned(16))) uint8_t tailb[I8 ? 2 * Lds::kTile : 16];  // the open block's rows
     const AttnArgs &a = pa.a;
     const PoolGeom &g = a.g;
@@ -1428,7 +1429,9 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         // the four lanes of a row.
         // the bf16 stage buffer the MFMAs read for stage st
         auto stage_buf = [&](int st) -> uint8_t * {
-            if constexpr (Q8)
+            if constexpr (I8)
+                return &bfs[st & 3][0];
+            else if constexpr (F8)
                 return &bfs[st & 1][0];
             else
                 return &ring[st % kPfStages][0];
@@ -1534,7 +1537,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         // st - 1, which both groups finished before reaching it.  The fp8
         // kernel keeps the common barrier: its conversion step is a second
         // workgroup-wide exchange per stage.
-        constexpr bool kPP = !Q8;
+        constexpr bool kPP = !F8;
         if constexpr (I8)
             if (tail_v >= 0 && tid < 4 * D) ((uint4 *)tailb)[tid] = tail_part;
         // a landed stage -> bf16
@@ -1546,16 +1549,30 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                                     tail_v >= 0 && tail_v / 2 == st ? tail_v & 1 : -1, tailb);
         };
         // int8: {K, V} scale of this lane's block in stage st, from its ring slot
-        // (which the stage's own step may still read)
+        // (which the stage's own step may still read); 1 for the tail and past the
+        // segment's last block
+        const int coded_end = tail_v >= 0 ? tail_v : seg_nvb;
         auto scales = [&](int st) __attribute__((always_inline)) {
             const float2 x = *(const float2 *)(&ring[st % kPfStages][0] + lblk * kI8Blk + kI8Codes);
-            return 2 * st + lblk == tail_v ? make_float2(1.f, 1.f) : x;
+            return 2 * st + lblk < coded_end ? x : make_float2(1.f, 1.f);
         };
         const bool grp_b = kPP && wv >= kPfWaves / 2;
-        if (dma_wave) vm_wait<NPW * (kPfStages - (kPP ? 3 : 2))>();  // stage 0 (and 1) landed
+        // Int8 converts a stage three iterations before its step, into one of four
+        // bf16 buffers, beside the PV MFMAs of the iteration's own stage: one barrier
+        // a stage, met by the two groups of waves as by bf16's, and V read only
+        // once the K fragments' registers are free.  128 sessions of G = 8, 25 tokens,
+        // per layer: 343 us with the FP8 kernel's two buffers and two barriers
+        // (five registers spilled), 309 converting one stage ahead, 305 with the
+        // conversion between the MFMAs, 279 with the groups apart.
+        constexpr int kAhead = I8 ? 2 : kPP ? 1 : 0;  // stages that land further ahead
+        if (dma_wave) vm_wait<NPW * (kPfStages - 2 - kAhead)>();  // stage 0 (and 1) landed
         __syncthreads();
         if constexpr (Q8) {
             convert(0);
+            if constexpr (I8) {
+                convert(1);
+                convert(2);
+            }
             __syncthreads();
         }
         // one stage; MASKED: the stage may hold keys some row cannot see
@@ -1565,32 +1582,41 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             const uint8_t *sm = stage_buf(st);
             // V^T chunks of stage st (visible since the previous barrier):
             // their LDS latency overlaps the wait below
+            // (int8: after the conversion, which needs the registers)
             uint4 vf[NT16];
+            auto load_vf = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int dt = 0; dt < NT16; ++dt) vf[dt] = *(const uint4 *)(sm + voff + dt * 16 * 32);
-            float v_scale = 1.f;
+                for (int dt = 0; dt < NT16; ++dt) vf[dt] = *(const uint4 *)(sm + voff + dt * 16 * 32);
+                if constexpr (MASKED) {
+                    uint32_t vm[4];
+                    v_slot_mask(st, vm);
+#pragma unroll
+                    for (int dt = 0; dt < NT16; ++dt)
+                        vf[dt] = make_uint4(vf[dt].x & vm[0], vf[dt].y & vm[1], vf[dt].z & vm[2], vf[dt].w & vm[3]);
+                }
+            };
+            if constexpr (!I8) load_vf();
+            // int8: the scores are of codes, to be multiplied by k_scale; the V scale
+            // enters the probabilities through their exponent.  One fused
+            // multiply-add per score does both and takes the reference off
+            // (128 sessions of G = 8 350 us a layer with the products apart, 343 so,
+            // before the stages overlapped).  A NaN scale makes even unseen rows NaN
+            // here; those tiles are computed apart below.
+            float k_scale = 1.f, v_log = 0.f, v_inv = 1.f;
             if constexpr (I8) {
                 const float2 x = scales(st);
-                v_scale = x.y;
-#pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    sa[i] *= x.x;
-                    sb[i] *= x.x;
-                }
+                k_scale = x.x;
+                v_log = __builtin_amdgcn_logf(x.y);
+                v_inv = __builtin_amdgcn_exp2f(-v_log);
             }
             if constexpr (MASKED) {
                 mask_scores(nt_c, st, sa, sb);
-                uint32_t vm[4];
-                v_slot_mask(st, vm);
-#pragma unroll
-                for (int dt = 0; dt < NT16; ++dt)
-                    vf[dt] = make_uint4(vf[dt].x & vm[0], vf[dt].y & vm[1], vf[dt].z & vm[2], vf[dt].w & vm[3]);
             }
             // stage st + 1 (ping-pong: st + 2) landed (zero-page stages after
             // the last); the barrier covers both DMA waves and frees the ring
             // slot last read at st - 1, which takes stage st + kPfStages - 1
             if (!grp_b) {
-                if (dma_wave) vm_wait<NPW * (kPfStages - (kPP ? 4 : 3))>();
+                if (dma_wave) vm_wait<NPW * (kPfStages - 3 - kAhead)>();
                 __syncthreads();
                 if (dma_wave) {
                     const int nst = st + kPfStages - 1;
@@ -1598,7 +1624,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                     nph = phys(2 * (nst + 1) + db);
                 }
             }
-            if constexpr (Q8) {
+            if constexpr (F8) {
                 // the other bf16 buffer: its stage (st - 1) is consumed
                 convert(st + 1);
                 __syncthreads();
@@ -1625,6 +1651,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 // compiler two NaN-quieting instructions); sa[i][0] twice
                 m8[i] = vmax3(vmax3(sa[i][0], sa[i][1], sa[i][2]), vmax3(sa[i][3], sb[i][0], sb[i][1]),
                               vmax3(sb[i][2], sb[i][3], sa[i][0]));
+                if constexpr (I8) m8[i] *= k_scale;
                 bump = bump || m8[i] > thr[i];
             }
             // (D = 64, whose references move in most stages: a test for each tile)
@@ -1666,6 +1693,9 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             f32x4_t na[kPfTpw], nb[kPfTpw];
             float p[kPfTpw][8];
             constexpr int kEpg = 8 * NT / ND;  // probabilities per group
+            float ex[kPfTpw];                  // int8: added to the scaled scores
+#pragma unroll
+            for (int i = 0; i < NT; ++i) ex[i] = v_log - m_ref[i];
 #pragma unroll
             for (int s = 0; s < ND; ++s) {
 #pragma unroll
@@ -1678,7 +1708,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 for (int u = 0; u < kEpg; ++u) {
                     const int f = s * kEpg + u, i = f >> 3, e = f & 7;
                     const float sc = e < 4 ? sa[i][e] : sb[i][e - 4];
-                    p[i][e] = __builtin_amdgcn_exp2f(kShift ? sc : sc - m_ref[i]);
+                    p[i][e] = __builtin_amdgcn_exp2f(I8 ? fmaf(sc, k_scale, ex[i]) : kShift ? sc : sc - m_ref[i]);
                     // keep it in this group: without the pin the compiler sinks every
                     // exponential below the last group, after the QK MFMAs
                     asm volatile("" : "+v"(p[i][e]));
@@ -1693,16 +1723,17 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 __builtin_amdgcn_sched_barrier(0);
 #endif
             }
+            if constexpr (I8) {
+                if (grp_b) __syncthreads();
+                load_vf();
+                convert(st + 3);  // over stage st - 1
+            }
             uint4 pb[kPfTpw];
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                float w[8];  // probabilities, int8: times the V scale
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = I8 ? p[i][e] * v_scale : p[i][e];
-                pb[i] = make_uint4(pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]),
-                                   pack_bf16x2(w[6], w[7]));
-            }
-            if (grp_b) __syncthreads();  // group B's stage barrier
+            for (int i = 0; i < NT; ++i)  // (int8: times the V scale)
+                pb[i] = make_uint4(pack_bf16x2(p[i][0], p[i][1]), pack_bf16x2(p[i][2], p[i][3]),
+                                   pack_bf16x2(p[i][4], p[i][5]), pack_bf16x2(p[i][6], p[i][7]));
+            if (!I8 && grp_b) __syncthreads();  // group B's stage barrier
             // row sums: of the bf16 probabilities by an all-ones A operand, or
             // the lane's part by vector adds
             const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
@@ -1710,6 +1741,9 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             for (int i = 0; i < NT; ++i) {
                 if constexpr (kMfmaSum)
                     l_i[i] = mfma16x16x32(ones, pb[i], l_i[i]);
+                else if constexpr (I8)
+                    ls[i] = fmaf(((p[i][0] + p[i][1]) + (p[i][2] + p[i][3])) +
+                                     ((p[i][4] + p[i][5]) + (p[i][6] + p[i][7])), v_inv, ls[i]);
                 else
                     ls[i] += ((p[i][0] + p[i][1]) + (p[i][2] + p[i][3])) +
                              ((p[i][4] + p[i][5]) + (p[i][6] + p[i][7]));
@@ -1718,6 +1752,14 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             for (int dt = 0; dt < NT16; ++dt) {
 #pragma unroll
                 for (int i = 0; i < NT; ++i) acc[i][dt] = mfma16x16x32(vf[dt], pb[i], acc[i][dt]);
+            }
+            if constexpr (I8) {  // the conversion's arithmetic between the MFMAs
+                __builtin_amdgcn_sched_group_barrier(0x100, NT16 + 4, 0);
+#pragma unroll
+                for (int k = 0; k < NT16 * NT; ++k) {
+                    __builtin_amdgcn_sched_group_barrier(0x002, 4 / NT, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                }
             }
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
@@ -1798,15 +1840,15 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 int vlo, vhi;
                 row_slots(mb, tq_i[i], vlo, vhi);
                 const bool in_tail = I8 && 2 * st + lblk == tail_v;
-                float v_scale = 1.f;
+                float k_scale = 1.f, v_scale = 1.f;
                 if constexpr (I8) {
                     if (!in_tail && (lblk ? ph1 : ph0) >= 0) {
                         const float2 x = *(const float2 *)(vb + kI8Codes);
-                        s0 *= x.x;
-                        s1 *= x.x;
+                        k_scale = x.x;
                         v_scale = x.y;
                     }
                 }
+                const float v_log = I8 ? __builtin_amdgcn_logf(v_scale) : 0.f;
                 float sc[8], p[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -1815,7 +1857,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 }
                 const float m8 = vmax3(vmax3(sc[0], sc[1], sc[2]), vmax3(sc[3], sc[4], sc[5]),
                                        vmax3(sc[6], sc[7], sc[0]));
-                const float mx = rows_max(m8) + msh[i];
+                const float mx = rows_max(I8 ? m8 * k_scale : m8) + msh[i];
                 const bool up = mx > m_ref[i] + kLazy;
                 // (a branch as in the stage loop: in one block the compiler may fuse
                 // the rescale into the sums)
@@ -1835,16 +1877,24 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                     for (int dt = 0; dt < NT16; ++dt) acc[i][dt] *= alpha;
                 }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(kShift ? sc[e] : sc[e] - m_ref[i]);
-                float w[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e)  // (an unseen block's scale may be NaN)
-                    w[e] = !I8 ? p[e] : lkey0 + e >= vlo && lkey0 + e < vhi ? p[e] * v_scale : 0.f;
-                const uint4 pb = make_uint4(pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]),
-                                            pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7]));
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (I8) {
+                        p[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], k_scale, v_log - m_ref[i]));
+                        // (an unseen block's scales may be NaN)
+                        p[e] = lkey0 + e >= vlo && lkey0 + e < vhi ? p[e] : 0.f;
+                    } else {
+                        p[e] = __builtin_amdgcn_exp2f(kShift ? sc[e] : sc[e] - m_ref[i]);
+                    }
+                }
+                const uint4 pb = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]),
+                                            pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
                 if constexpr (kMfmaSum)
                     l_i[i] = mfma16x16x32(make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u),
                                           pb, l_i[i]);
+                else if constexpr (I8)
+                    ls[i] = vlo < vhi ? fmaf(((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])),
+                                             __builtin_amdgcn_exp2f(-v_log), ls[i])
+                                      : ls[i];
                 else
                     ls[i] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
 #pragma nounroll
