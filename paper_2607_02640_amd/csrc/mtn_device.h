@@ -372,6 +372,26 @@ __device__ __forceinline__ f32x4_t mfma16x16x32(const uint4 &a, const uint4 &b, 
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
                                                     __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
+// The same over f16, which holds int8 codes exactly and a query in 11 bits.
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
+__device__ __forceinline__ f32x4_t mfma16x16x32_f16(const uint4 &a, const uint4 &b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a),
+                                                  __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    const f16x2_t v = {(_Float16)lo, (_Float16)hi};
+    return __builtin_bit_cast(uint32_t, v);
+}
+// Int8 codes stored plus 128 (bytes 2H, 2H + 1 of w) as two f16, exact: the bytes
+// under 0x64 are 1024 + u, from which 1024 + 128 is taken off.
+template <bool H>
+__device__ __forceinline__ uint32_t i8_f16x2(uint32_t w) {
+    const f16x2_t u = __builtin_bit_cast(
+        f16x2_t, __builtin_amdgcn_perm(0x64646464u, w, H ? 0x04030402u : 0x04010400u));
+    const f16x2_t off = {(_Float16)-1152.f, (_Float16)-1152.f};
+    return __builtin_bit_cast(uint32_t, u + off);
+}
 // Maxima written as ordinary code, so that the compiler sees every read of
 // a matrix-instruction result and spaces it as the hardware requires (inline
 // assembly reading an MFMA accumulator is issued with no wait states).  Three

@@ -33,30 +33,11 @@
 namespace mtn {
 namespace {
 
-typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
-typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 
-__device__ __forceinline__ f32x4_t mfma_qk_f16(const uint4 &a, const uint4 &b, f32x4_t c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a),
-                                                  __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
-}
 __device__ __forceinline__ f32x4_t mfma_pv16(const uint2 &a, const uint2 &b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, a),
                                                       __builtin_bit_cast(s16x4_t, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
-    const f16x2_t v = {(_Float16)lo, (_Float16)hi};
-    return __builtin_bit_cast(uint32_t, v);
-}
-// K codes (bytes 2H, 2H + 1 of w, biased) as two f16, exact: the bytes under
-// 0x64 are 1024 + u, from which 1024 + 128 is taken off
-template <bool H>
-__device__ __forceinline__ uint32_t k_f16x2(uint32_t w) {
-    const f16x2_t u = __builtin_bit_cast(
-        f16x2_t, __builtin_amdgcn_perm(0x64646464u, w, H ? 0x04030402u : 0x04010400u));
-    const f16x2_t off = {(_Float16)-1152.f, (_Float16)-1152.f};
-    return __builtin_bit_cast(uint32_t, u + off);
 }
 // codes of a row or block: nearest integer to x / s (the correctly rounded
 // quotient), within [-127, 127]
@@ -583,8 +564,8 @@ __global__ __launch_bounds__(64 * kI8Waves) void k_attn_i8(I8Args ia) {
         f32x4_t c = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < ND; ++s)
-            c = mfma_qk_f16(make_uint4(k_f16x2<false>(kw[2 * s]), k_f16x2<true>(kw[2 * s]),
-                                       k_f16x2<false>(kw[2 * s + 1]), k_f16x2<true>(kw[2 * s + 1])), qh[s], c);
+            c = mfma16x16x32_f16(make_uint4(i8_f16x2<false>(kw[2 * s]), i8_f16x2<true>(kw[2 * s]),
+                                       i8_f16x2<false>(kw[2 * s + 1]), i8_f16x2<true>(kw[2 * s + 1])), qh[s], c);
         const float ks = sc2.x * qscale;
         float sc[4];
         bool ok[4] = {true, true, true, true};

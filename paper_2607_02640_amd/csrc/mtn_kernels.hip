@@ -928,15 +928,14 @@ __device__ __forceinline__ uint2 i8_bf16x4(uint32_t w) {
     return make_uint2(__builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u),
                       __builtin_amdgcn_perm(__float_as_uint(f3), __float_as_uint(f2), 0x07060302u));
 }
-// ... eight K codes (stored plus 128) of a row
+// ... eight K codes (stored plus 128) of a row as f16
 __device__ __forceinline__ uint4 i8_keys(const uint2 &c) {
-    const uint2 a = i8_bf16x4(c.x ^ 0x80808080u), b = i8_bf16x4(c.y ^ 0x80808080u);
-    return make_uint4(a.x, a.y, b.x, b.y);
+    return make_uint4(i8_f16x2<false>(c.x), i8_f16x2<true>(c.x), i8_f16x2<false>(c.y), i8_f16x2<true>(c.y));
 }
 // An int8 stage (two regions of `blk` bytes: K codes, V codes in key quads, 16
-// bytes with the scales) -> the bf16 stage layout, codes as they are: the scales
-// are applied to scores and probabilities.  Block tail_b (or none) comes from
-// `tail`, K [16][D] and V [16][D] bf16.  512 threads, 256 per block: K dims 8 hc .. + 7
+// bytes with the scales) -> the bf16 stage layout, K codes in f16 and V codes in
+// bf16 as they are: the scales are applied to scores and probabilities.  Block
+// tail_b (or none) comes from `tail`, K [16][D] f16 (scaled) and V [16][D] bf16.  512 threads, 256 per block: K dims 8 hc .. + 7
 // of a key, and V dims 2 dp, 2 dp + 1 of a key quad, D = 64 one of the two.
 template <int D>
 __device__ __forceinline__ void i8_stage_to_bf16(const uint8_t *src, int blk, uint8_t *dst, int tid, int tail_b,
@@ -990,6 +989,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
     __shared__ __attribute__((aligned(16))) uint8_t ring[kPfStages][SB];
     __shared__ __attribute__((aligned(16))) uint8_t bfs[I8 ? 4 : F8 ? 2 : 1][Q8 ? Lds::kStage : 16];
     __shared__ __attribute__((aligned(16))) uint8_t tailb[I8 ? 2 * Lds::kTile : 16];  // the open block's rows
+    __shared__ float tail_max[I8 ? kPfWaves : 1];
     const AttnArgs &a = pa.a;
     const PoolGeom &g = a.g;
     // one workgroup per (sequence, row pass, kv head, key segment): a long
@@ -1049,7 +1049,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
     const int seg_nvb = min(nvb - vb0, 2 * n_stages);  // blocks of the segment
     // int8: the union's last block, if the plan leaves it open, lies in the
     // session's tail: its number in the segment, or -1
-    int tail_v = -1;
+    int tail_v = -1, tail_n = 0;  // ... and its rows
     const uint8_t *tail_rows = nullptr;
     if constexpr (I8) {
         const int lp = pos0 + ntok - 1;  // the plan's last position
@@ -1057,6 +1057,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         const int rows = lp < g.n_sink ? min(kBlock, g.n_sink - (lp - lo)) : kBlock;
         if (lo + 1 < rows && tq_max >= lp - lo && nvb - 1 >= vb0 && nvb - 1 - vb0 < seg_nvb) {
             tail_v = nvb - 1 - vb0;
+            tail_n = lo + 1;
             tail_rows = pa.tails.base + ((int64_t)sid * 2 + scalar_ld(rec, 6)) * pa.tails.stride +
                         ((int64_t)a.layer * g.hkv + kvh) * (64 * D);
         }
@@ -1378,8 +1379,27 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
 #pragma unroll
                 for (int s = 0; s < ND; ++s) rope_split(qx[i][s], qy[i][s], s >= ND / 2);
         }
+        // int8: the query in f16 (against exact codes: 11 bits where bf16 has 8), each
+        // row scaled by a power of two that its elements' largest magnitude gives;
+        // the rotation adds less than a bit, the form's magnitude few more
+        float q_sc[kPfTpw];
 #pragma unroll
         for (int i = 0; i < kPfTpw; ++i) {
+            q_sc[i] = 1.f;
+            float q_mul = a.scale_log2;
+            if constexpr (I8) {
+                float mx = 0.f;
+#pragma unroll
+                for (int s = 0; s < ND; ++s) {
+                    float x[8];
+                    unpack8(qx[i][s], x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(x[e]));
+                }
+                const int eq = max(__builtin_amdgcn_frexp_expf(rows_max(mx) * a.scale_log2) + 1, -100);
+                q_sc[i] = ldexpf(1.f, eq);
+                q_mul = ldexpf(a.scale_log2, -eq);
+            }
 #pragma unroll
             for (int s = 0; s < ND; ++s) {
                 // dims d0 + e, e < 8, d0 = s*32 + 8*lg; RoPE partner is d +- D / 2
@@ -1406,8 +1426,8 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
 #pragma unroll
                     for (int u = 0; u < 2; ++u)
                         r2[u] = fmaf(xv[e + u], cs[2 * (e + u)], sg * yv[e + u] * cs[2 * (e + u) + 1]) *
-                                a.scale_log2;
-                    w[e / 2] = pack_bf16x2(r2[0], r2[1]) & keep;
+                                (I8 ? q_mul : a.scale_log2);
+                    w[e / 2] = (I8 ? pack_f16x2(r2[0], r2[1]) : pack_bf16x2(r2[0], r2[1])) & keep;
                 }
                 // computed here, before the DMA waves issue the ring: the
                 // compiler's waits for these loads count only its own loads, so
@@ -1480,6 +1500,12 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         // S^T of a stage for every tile of this wave (K fragments read once,
         // shared by the tiles; tiles past the last row compute on zero
         // queries and are dropped)
+        auto qk_mfma = [&](const uint4 &k, const uint4 &q, f32x4_t c) __attribute__((always_inline)) {
+            if constexpr (I8)
+                return mfma16x16x32_f16(k, q, c);
+            else
+                return mfma16x16x32(k, q, c);
+        };
         auto qk = [&](auto nt_c, const uint8_t *sm, f32x4_t (&sa)[kPfTpw], f32x4_t (&sb)[kPfTpw])
                       __attribute__((always_inline)) {
             constexpr int NT = decltype(nt_c)::value;
@@ -1494,8 +1520,8 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 const uint4 k1 = *(const uint4 *)(sm + koff[s] + 4 * Lds::kRow);
 #pragma unroll
                 for (int i = 0; i < NT; ++i) {
-                    sa[i] = mfma16x16x32(k0, qf[i][s], sa[i]);
-                    sb[i] = mfma16x16x32(k1, qf[i][s], sb[i]);
+                    sa[i] = qk_mfma(k0, qf[i][s], sa[i]);
+                    sb[i] = qk_mfma(k1, qf[i][s], sb[i]);
                 }
             }
         };
@@ -1538,8 +1564,33 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         // kernel keeps the common barrier: its conversion step is a second
         // workgroup-wide exchange per stage.
         constexpr bool kPP = !F8;
-        if constexpr (I8)
-            if (tail_v >= 0 && tid < 4 * D) ((uint4 *)tailb)[tid] = tail_part;
+        // The open block's K rows in f16 as the codes are, scaled by a power of two
+        // from their largest finite magnitude (eight bits of each stay, down to 2^-16
+        // of it): threads 0 .. 2 D - 1 hold them, eight elements each, row by row.
+        float tail_scale = 1.f;
+        if constexpr (I8) {
+            if (tail_v >= 0) {
+                float x[8], mx = 0.f;
+                unpack8(tail_part, x);
+                if (tid < 2 * D && tid / (D / 8) < tail_n)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) mx = fabsf(x[e]) < INFINITY ? fmaxf(mx, fabsf(x[e])) : mx;
+#pragma unroll
+                for (int m = 1; m < 64; m <<= 1) mx = fmaxf(mx, __shfl_xor(mx, m, 64));
+                if (lane == 0) tail_max[wv] = mx;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < kPfWaves; ++w) mx = fmaxf(mx, tail_max[w]);
+                const int et = min(__builtin_amdgcn_frexp_expf(mx), 127);
+                tail_scale = ldexpf(1.f, et);
+                if (tid < 2 * D)
+                    tail_part = make_uint4(pack_f16x2(ldexpf(x[0], -et), ldexpf(x[1], -et)),
+                                           pack_f16x2(ldexpf(x[2], -et), ldexpf(x[3], -et)),
+                                           pack_f16x2(ldexpf(x[4], -et), ldexpf(x[5], -et)),
+                                           pack_f16x2(ldexpf(x[6], -et), ldexpf(x[7], -et)));
+                if (tid < 4 * D) ((uint4 *)tailb)[tid] = tail_part;
+            }
+        }
         // a landed stage -> bf16
         auto convert = [&](int st) __attribute__((always_inline)) {
             if constexpr (F8)
@@ -1549,12 +1600,12 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                                     tail_v >= 0 && tail_v / 2 == st ? tail_v & 1 : -1, tailb);
         };
         // int8: {K, V} scale of this lane's block in stage st, from its ring slot
-        // (which the stage's own step may still read); 1 for the tail and past the
+        // (which the stage's own step may still read); the tail's own, and any past the
         // segment's last block
         const int coded_end = tail_v >= 0 ? tail_v : seg_nvb;
         auto scales = [&](int st) __attribute__((always_inline)) {
             const float2 x = *(const float2 *)(&ring[st % kPfStages][0] + lblk * kI8Blk + kI8Codes);
-            return 2 * st + lblk < coded_end ? x : make_float2(1.f, 1.f);
+            return 2 * st + lblk < coded_end ? x : make_float2(tail_scale, 1.f);
         };
         const bool grp_b = kPP && wv >= kPfWaves / 2;
         // Int8 converts a stage three iterations before its step, into one of four
@@ -1651,7 +1702,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 // compiler two NaN-quieting instructions); sa[i][0] twice
                 m8[i] = vmax3(vmax3(sa[i][0], sa[i][1], sa[i][2]), vmax3(sa[i][3], sb[i][0], sb[i][1]),
                               vmax3(sb[i][2], sb[i][3], sa[i][0]));
-                if constexpr (I8) m8[i] *= k_scale;
+                if constexpr (I8) m8[i] *= k_scale * q_sc[i];
                 bump = bump || m8[i] > thr[i];
             }
             // (D = 64, whose references move in most stages: a test for each tile)
@@ -1693,22 +1744,25 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             f32x4_t na[kPfTpw], nb[kPfTpw];
             float p[kPfTpw][8];
             constexpr int kEpg = 8 * NT / ND;  // probabilities per group
-            float ex[kPfTpw];                  // int8: added to the scaled scores
+            float ex[kPfTpw], kq[kPfTpw];      // int8: added to the scores, their scale
 #pragma unroll
-            for (int i = 0; i < NT; ++i) ex[i] = v_log - m_ref[i];
+            for (int i = 0; i < NT; ++i) {
+                ex[i] = v_log - m_ref[i];
+                kq[i] = k_scale * q_sc[i];
+            }
 #pragma unroll
             for (int s = 0; s < ND; ++s) {
 #pragma unroll
                 for (int i = 0; i < NT; ++i) {
                     const f32x4_t c0 = kShift ? csh[i] : f32x4_t{0.f, 0.f, 0.f, 0.f};
-                    na[i] = mfma16x16x32(kf[s][0], qf[i][s], s ? na[i] : c0);
-                    nb[i] = mfma16x16x32(kf[s][1], qf[i][s], s ? nb[i] : c0);
+                    na[i] = qk_mfma(kf[s][0], qf[i][s], s ? na[i] : c0);
+                    nb[i] = qk_mfma(kf[s][1], qf[i][s], s ? nb[i] : c0);
                 }
 #pragma unroll
                 for (int u = 0; u < kEpg; ++u) {
                     const int f = s * kEpg + u, i = f >> 3, e = f & 7;
                     const float sc = e < 4 ? sa[i][e] : sb[i][e - 4];
-                    p[i][e] = __builtin_amdgcn_exp2f(I8 ? fmaf(sc, k_scale, ex[i]) : kShift ? sc : sc - m_ref[i]);
+                    p[i][e] = __builtin_amdgcn_exp2f(I8 ? fmaf(sc, kq[i], ex[i]) : kShift ? sc : sc - m_ref[i]);
                     // keep it in this group: without the pin the compiler sinks every
                     // exponential below the last group, after the QK MFMAs
                     asm volatile("" : "+v"(p[i][e]));
@@ -1833,8 +1887,8 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                         else
                             k2[x] = ((const uint4 *)(kb + key * Lds::kRow))[s * 4 + lg];
                     }
-                    s0 = mfma16x16x32(k2[0], qf[i][s], s0);
-                    s1 = mfma16x16x32(k2[1], qf[i][s], s1);
+                    s0 = qk_mfma(k2[0], qf[i][s], s0);
+                    s1 = qk_mfma(k2[1], qf[i][s], s1);
                 }
                 const PfBlock mb = vblock(2 * st + lblk);
                 int vlo, vhi;
@@ -1846,7 +1900,10 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                         const float2 x = *(const float2 *)(vb + kI8Codes);
                         k_scale = x.x;
                         v_scale = x.y;
+                    } else {
+                        k_scale = tail_scale;
                     }
+                    k_scale *= q_sc[i];
                 }
                 const float v_log = I8 ? __builtin_amdgcn_logf(v_scale) : 0.f;
                 float sc[8], p[8];
