@@ -68,9 +68,10 @@ def parse():
     ap.add_argument("--cpu-frames", type=int, default=2,
                     help="consecutive session-frames each oracle process times")
     ap.add_argument("--n-split", type=int, default=0)
-    ap.add_argument("--kv-dtype", choices=["bf16", "fp8"], default=None,
+    ap.add_argument("--kv-dtype", choices=["bf16", "fp8", "int8"], default=None,
                     help="KV cache element type (default: the workload's); fp8 keeps E4M3 "
-                         "codes with per-token power-of-two scales and bf16 io")
+                         "codes with per-token power-of-two scales, int8 int8 codes with a "
+                         "scale per block of 16 tokens and head, both with bf16 io")
     ap.add_argument("--json-out", default=None)
     ap.add_argument("--call", action="store_true",
                     help="run a whole simulated call from empty sessions and report the "
@@ -144,6 +145,12 @@ def kernel_src_hash(kernel: str = "decode") -> str:
     return h.hexdigest()[:16]
 
 
+def token_bytes(kvd, Hkv, D):
+    """Pool bytes of one token: K and V of every head, and the scales: fp8 one
+    byte per row, int8 a float for each tensor of a block of 16 tokens."""
+    return Hkv * {"f32": 8 * D, "bf16": 4 * D, "fp8": 2 * D + 2, "int8": 2 * D + 0.5}[kvd]
+
+
 def algorithmic_bytes(w, kvd="bf16", fused_append=None):
     """Per-launch algorithmic bytes of the steady-state decode and chunk
     prefill of workload w (every query sees S + W keys).  Both launches may
@@ -156,11 +163,11 @@ def algorithmic_bytes(w, kvd="bf16", fused_append=None):
     N, Hq, Hkv, D = w.n_sessions, w.n_q_heads, w.n_kv_heads, w.head_dim
     C = w.chunk[1]
     vis = w.n_sink + w.window
-    beta = Hkv * (2 * D + 2) if kvd == "fp8" else 2 * Hkv * D * esz
+    beta = token_bytes(kvd, Hkv, D)
     app = 2 * Hkv * D * esz + beta                       # one token's append
     dec = N * (vis * beta + Hq * D * 2 * esz + app)
     pre = N * ((vis + C - 1) * beta + C * Hq * D * 2 * esz + (C * app if fused_append else 0))
-    return dec, pre
+    return round(dec), round(pre)
 
 
 def traffic_summary(fetch_dir, write_dir):
@@ -354,8 +361,8 @@ def run_gpu(args, w):
     # per launch like the decode: a launch that only streamed its bytes, with
     # no fixed cost beyond one kernel's start and drain
     vis = w.n_sink + w.window
-    beta = Hkv * (2 * D + 2) if kvd == "fp8" else 2 * Hkv * D * esz
-    dec_bytes_est = N * (vis * beta + Hq * D * 2 * esz + 2 * Hkv * D * esz + beta)
+    beta = token_bytes(kvd, Hkv, D)
+    dec_bytes_est = int(N * (vis * beta + Hq * D * 2 * esz + 2 * Hkv * D * esz + beta))
     same_bytes = min(READ_PROBE_BYTES, dec_bytes_est // 8192 * 8192)
     mtn.hbm_read(rsrc, same_bytes)
     pairs = [(torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True))
@@ -411,8 +418,7 @@ def run_gpu(args, w):
     # launch also appends its token (read k, v; write the pool copy), and so
     # does a chunk prefill with the append fused in (no append launches in the
     # timed frames)
-    # pool bytes of one token (all kv heads): K and V rows, plus the two scale
-    # exponent bytes per head of the fp8 cache
+    # pool bytes of one token (all kv heads)
     n_dec, ms_dec = kt["decode"]
     # merges of decode segments; those of chunk segments belong to the prefill
     n_mrg, ms_mrg = (x - y for x, y in zip(kt["merge"], kt["prefill_merge"]))
@@ -420,7 +426,7 @@ def run_gpu(args, w):
     ms_pre += kt["prefill_merge"][1]
     n_app, ms_app = kt["append"]
     vis = w.n_sink + w.window
-    beta = Hkv * (2 * D + 2) if kvd == "fp8" else 2 * Hkv * D * esz
+    beta = token_bytes(kvd, Hkv, D)
     app_tok = 2 * Hkv * D * esz + beta
     # per decode launch: the visible keys, q in and out, the new token's k and v
     # in (io type) and its pool copy out
@@ -1072,11 +1078,13 @@ def main():
             "decode_steps": w.n_decode[1], "frame_budget_s": w.frame_period_s,
             "steady_state": "every query sees S + W keys", "parallelism": "single GPU",
             "kv_cache": {"bf16": "bf16", "f32": "fp32",
-                         "fp8": "fp8-e4m3, per-token power-of-two scales"}[res["kv_dtype"]],
+                         "fp8": "fp8-e4m3, per-token power-of-two scales",
+                         "int8": "int8, fp32 scale per block of 16 tokens and head"}[res["kv_dtype"]],
         },
         "roofline": {
             "bound": "hbm",
             "kernel": ("decode attention (k_attn_mfma, fp8 blocks)" if res["kv_dtype"] == "fp8"
+                       else "decode attention (k_attn_i8, int8 blocks)" if res["kv_dtype"] == "int8"
                        else "decode attention (k_attn_mfma, bf16 blocks)"
                        if w.n_q_heads == 8 * w.n_kv_heads and w.head_dim == 128
                        else "decode attention (k_attn_valu)"),
@@ -1085,7 +1093,7 @@ def main():
             "unit": "GB/s",
             "frac": round(res["dec_gbps"] / HBM_PEAK_GBPS, 4),
             "traffic": measured_traffic(args.workload) if res["kv_dtype"] == w.dtype else None,
-            "bytes_per_launch": res["dec_bytes"],
+            "bytes_per_launch": round(res["dec_bytes"]),
             "avg_launch_ms": round(res["avg_dec_ms"], 4),
             "launches": res["dec_launches"],
         },
