@@ -590,7 +590,8 @@ mtn_status copy_tails(mtn_pool *P, const TailView &from, const TailView &to,
 
 // The fork's device work: the source's pages into the blocks that the copies'
 // table rows name, and those rows.
-mtn_status fork_pages(mtn_pool *P, int32_t src, const std::vector<int32_t> &sids, hipStream_t s) {
+mtn_status fork_pages(mtn_pool *P, int32_t src, const std::vector<int32_t> &sids,
+                      const std::vector<std::pair<int32_t, int32_t>> &tail_slots, hipStream_t s) {
     const int32_t pages = P->n_assigned[src];
     ForkArgs a;
     a.kv = P->kv;
@@ -613,12 +614,7 @@ mtn_status fork_pages(mtn_pool *P, int32_t src, const std::vector<int32_t> &sids
             HIP_TRY(P, launch_fork(a, P->cfg.n_layers, s));
         }
     }
-    if (P->int8 && open_rows(P, P->len[src])) {
-        std::vector<std::pair<int32_t, int32_t>> slots;
-        for (const int32_t c : sids) slots.emplace_back(2 * src + P->tail[src], 2 * c + P->tail[src]);
-        return copy_tails(P, tails(P), tails(P), slots, s);
-    }
-    return MTN_OK;
+    return copy_tails(P, tails(P), tails(P), tail_slots, s);
 }
 
 // Internal plan begin.  rows == nullptr packs io rows in plan order.
@@ -852,7 +848,7 @@ mtn_status check_rope(const mtn_pool_config &c, const mtn_rope_config &r) {
     if (r.rotary_dim % 16) return MTN_ERR_UNSUPPORTED;
     if (r.scaling < MTN_ROPE_SCALE_NONE || r.scaling > MTN_ROPE_SCALE_YARN) return MTN_ERR_INVALID_ARG;
     // (written so that NaN fails)
-    if (!(r.magnitude >= 0.0) || !std::isfinite(r.magnitude)) return MTN_ERR_INVALID_ARG;
+    if (!(r.magnitude >= 0.0) || r.magnitude > 1024.0) return MTN_ERR_INVALID_ARG;
     if (r.scaling != MTN_ROPE_SCALE_NONE && (!(r.factor >= 1.0) || !std::isfinite(r.factor)))
         return MTN_ERR_INVALID_ARG;
     const double rd = r.rotary_dim ? r.rotary_dim : c.head_dim;
@@ -1521,15 +1517,20 @@ mtn_status mtn_session_fork(mtn_pool *P, int32_t sid, int32_t n_copies, int32_t 
         sids.reserve((size_t)n_copies);
         for (int32_t i = 0; (int32_t)sids.size() < n_copies; ++i)
             if (!P->is_open[i]) sids.push_back(i);
+        std::vector<std::pair<int32_t, int32_t>> tail_slots;  // int8: the open block's rows
+        if (P->int8 && open_rows(P, P->len[sid]))
+            for (const int32_t c : sids)
+                tail_slots.emplace_back(2 * sid + P->tail[sid], 2 * c + P->tail[sid]);
         mtn_status st = launch_gate(P);
         if (!st) st = follow_last_stream(P, stream);
         if (st) return st;
+        // (nothing below allocates)
         for (const int32_t c : sids) {
             int32_t *row = &P->table[(size_t)c * P->row_len];
             for (int32_t i = 0; i < pages; ++i) row[page_lb(P, sid, i)] = (int32_t)P->alloc.take();
         }
         if (!P->host_only && pages) {
-            st = fork_pages(P, sid, sids, (hipStream_t)stream);
+            st = fork_pages(P, sid, sids, tail_slots, (hipStream_t)stream);
             if (st) {  // the blocks go back; what a launch wrote lies in free blocks
                 for (const int32_t c : sids) {
                     int32_t *row = &P->table[(size_t)c * P->row_len];
