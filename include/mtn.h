@@ -204,7 +204,7 @@ typedef struct {
     double  factor;        /* scaling: >= 1, finite (ignored with NONE)        */
     double  beta_fast;     /* YARN: turns over the trained context; 0 = 32     */
     double  beta_slow;     /* YARN: 0 = 1; 0 < beta_slow < beta_fast           */
-    double  magnitude;     /* >= 0, finite; 0 = by scaling                     */
+    double  magnitude;     /* 0 = by scaling, else up to 1024                  */
 } mtn_rope_config;
 
 /* Synchronises the stream of the pool's previous plan.  An all-zero config is

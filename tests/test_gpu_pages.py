@@ -120,6 +120,41 @@ def test_pages_are_copied_whole(hkv, d, layers, tokens):
     assert torch.equal(kv, after)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "int8"])
+def test_many_sessions_move(dtype):
+    """More sessions than one launch's arguments hold, of different lengths, with
+    holes between them: each returns after the move what it does before."""
+    n, d = 300, 64
+    kw = dict(n_layers=1, hq=2, hkv=1, d=d, S=3, W=40, cmax=20, max_sessions=n, dtype=dtype)
+    pool = make_pool(**kw, n_blocks=5 * n)
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    draw = lambda *s: torch.randn(s, generator=gen, device="cuda").bfloat16()
+    sids = [pool.session_open() for _ in range(n)]
+    for turn in range(5):
+        who = [s for s in sids if s % 5 <= turn]
+        nt = [1 + (7 * s + turn) % 20 for s in who]
+        pool.plan_begin(who, nt)
+        pool.frame_append_kv(0, draw(sum(nt), 1, d), draw(sum(nt), 1, d))
+        pool.plan_commit()
+        if turn == 3:
+            for s in sids[::11]:
+                pool.session_close(s)
+            sids = [s for s in sids if s % 11]
+    k, v, q = draw(len(sids), 1, d), draw(len(sids), 1, d), draw(len(sids), 2, d)
+
+    def answers():
+        out = torch.empty_like(q)
+        pool.plan_begin(sids, [1] * len(sids))
+        pool.attend_decode_append(0, k, v, q, out)
+        pool.plan_abort()  # asked again below
+        return out
+    want = answers()
+    old, kv = pool.kv, torch.empty_like(pool.kv)
+    pool.resize(pool.cfg.n_blocks, kv)
+    old.fill_(0xFF)
+    assert torch.equal(answers(), want)
+
+
 def test_plans_and_page_operations_on_different_streams():
     """Each call waits for the work of the one before it, whatever its stream."""
     h, rnd = _harness("bf16", 8, 1, 128), random.Random(4)

@@ -69,6 +69,7 @@ def test_scalings_move_the_frequencies_they_name():
     (dict(scaling="yarn", factor=4.0, original_len=64, beta_slow=-1.0), mtn.MTN_ERR_INVALID_ARG),
     (dict(magnitude=-1.0), mtn.MTN_ERR_INVALID_ARG),
     (dict(magnitude=math.nan), mtn.MTN_ERR_INVALID_ARG),
+    (dict(magnitude=1025.0), mtn.MTN_ERR_INVALID_ARG),
 ])
 def test_bad_forms_are_refused(kw, code):
     with pytest.raises(mtn.MtnError) as e:
