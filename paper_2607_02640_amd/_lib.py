@@ -291,6 +291,8 @@ class Pool:
     def resize(self, n_blocks: int, kv=None, stream=None) -> None:
         """Move every page into the buffer ``kv`` with ``n_blocks`` blocks; the
         pool then holds ``kv`` and no longer the buffer before it."""
+        if not self.host_only and kv is not None and not (kv.device == self.kv.device and kv.is_contiguous()):
+            raise MtnError(MTN_ERR_INVALID_ARG, "resize", "kv: not contiguous, or on another device")
         size = C.c_size_t(kv.numel() * kv.element_size() if kv is not None else 0)
         if self.kv is not None:  # torch may not hand the old buffer out before the copy has run
             import torch

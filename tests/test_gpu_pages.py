@@ -202,6 +202,8 @@ def test_bad_buffers_are_refused():
     n = h.pool.required_bytes
     for kv, blocks in [(None, h.pool.cfg.n_blocks), (h.pool.kv, h.pool.cfg.n_blocks),
                        (torch.empty(n - 256, dtype=torch.uint8, device="cuda"), h.pool.cfg.n_blocks),
+                       (torch.empty(n, dtype=torch.uint8), h.pool.cfg.n_blocks),
+                       (torch.empty(1, dtype=torch.uint8, device="cuda").expand(n), h.pool.cfg.n_blocks),
                        (torch.empty(n + 16, dtype=torch.uint8, device="cuda")[16:], h.pool.cfg.n_blocks)]:
         assert _code(lambda: h.pool.resize(blocks, kv)) == mtn.MTN_ERR_INVALID_ARG
     _frames(h, random.Random(6), 2)
