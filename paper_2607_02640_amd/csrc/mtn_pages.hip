@@ -26,6 +26,7 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 constexpr int kPageThreads = 256;
+constexpr int64_t kMaxGrid = UINT32_MAX / kPageThreads;  // a dimension's threads are counted in 32 bits
 // 16-byte loads in flight per thread.  One session of 48 layers (411 MB) forked:
 // 136 us with 2, 138 with 4 or 5, 200 with 8; 24 int8 sessions of 12 layers (1.15 GB)
 // moved: 381, 402 and 383, 727.
@@ -112,7 +113,7 @@ __global__ __launch_bounds__(kPageThreads) void k_copy_tails(TailArgs a, Parts p
 hipError_t launch_fork(const ForkArgs &a, int32_t n_layers, hipStream_t s) {
     const Parts p = page_parts(a.block_stride);
     const int64_t x = (int64_t)a.m * p.parts;
-    if (a.m < 1 || a.copies < 1 || a.copies > kForkCopies || a.m * a.copies > kForkBlocks || x > INT32_MAX ||
+    if (a.m < 1 || a.copies < 1 || a.copies > kForkCopies || a.m * a.copies > kForkBlocks || x > kMaxGrid ||
         n_layers > 65535 || a.block_stride % 16 || a.block_stride / 16 > INT32_MAX)
         return hipErrorInvalidValue;
     hipLaunchKernelGGL(k_fork, dim3((unsigned)x, (unsigned)n_layers), dim3(kPageThreads), 0, s, a, p);
@@ -124,7 +125,7 @@ hipError_t launch_move(const MoveArgs &a, int32_t n_layers, hipStream_t s) {
     int64_t pages = 0;
     for (int i = 0; i < a.n; ++i) pages = std::max<int64_t>(pages, a.s[i].pages);
     const int64_t x = pages * p.parts;
-    if (a.n < 1 || a.n > kMoveSessions || x < 1 || x > INT32_MAX || n_layers > 65535 ||
+    if (a.n < 1 || a.n > kMoveSessions || x < 1 || x > kMaxGrid || n_layers > 65535 ||
         a.block_stride % 16 || a.block_stride / 16 > INT32_MAX)
         return hipErrorInvalidValue;
     hipLaunchKernelGGL(k_move, dim3((unsigned)x, (unsigned)a.n, (unsigned)n_layers), dim3(kPageThreads), 0, s, a, p);
