@@ -55,6 +55,8 @@
  *     non-finite element).  Rows of a block that is still open read as they
  *     were appended (keys rotated, then rounded to bf16).  Every row is
  *     rounded to 8 bits once, and the same whatever plans brought it.
+ *     (A probability times a V scale may be taken for zero below 2^-126, so an
+ *     output is off by up to 127 * 2^-126 per key, whatever the values' size.)
  *     Accumulation is fp32; bf16 results are rounded to
  *     nearest-even.
  */

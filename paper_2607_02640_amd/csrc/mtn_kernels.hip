@@ -1646,18 +1646,18 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 }
             };
             if constexpr (!I8) load_vf();
-            // int8: the scores are of codes, to be multiplied by k_scale; the V scale
-            // enters the probabilities through their exponent.  One fused
-            // multiply-add per score does both and takes the reference off
-            // (128 sessions of G = 8 350 us a layer with the products apart, 343 so,
-            // before the stages overlapped).  A NaN scale makes even unseen rows NaN
-            // here; those tiles are computed apart below.
-            float k_scale = 1.f, v_log = 0.f, v_inv = 1.f;
+            // int8: the scores are of codes, to be multiplied by k_scale, which one fused
+            // multiply-add per score does as it takes the reference off.  The V
+            // scale multiplies the probabilities once their sum is taken: the sum is
+            // of the scores alone (as the exponent's other addend, taken out of the
+            // sum again, it cost 283 us a layer instead of 286 at 128 sessions of
+            // G = 8, and keys of small values their share of the sum).  A NaN scale
+            // makes even unseen rows NaN here; those tiles are computed apart below.
+            float k_scale = 1.f, v_scale = 1.f;
             if constexpr (I8) {
                 const float2 x = scales(st);
                 k_scale = x.x;
-                v_log = __builtin_amdgcn_logf(x.y);
-                v_inv = __builtin_amdgcn_exp2f(-v_log);
+                v_scale = x.y;
             }
             if constexpr (MASKED) {
                 mask_scores(nt_c, st, sa, sb);
@@ -1746,7 +1746,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             float ex[kPfTpw], kq[kPfTpw];      // int8: added to the scores, their scale
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
-                ex[i] = v_log - m_ref[i];
+                ex[i] = -m_ref[i];
                 kq[i] = k_scale * q_sc[i];
             }
 #pragma unroll
@@ -1783,9 +1783,13 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             }
             uint4 pb[kPfTpw];
 #pragma unroll
-            for (int i = 0; i < NT; ++i)  // (int8: times the V scale)
-                pb[i] = make_uint4(pack_bf16x2(p[i][0], p[i][1]), pack_bf16x2(p[i][2], p[i][3]),
-                                   pack_bf16x2(p[i][4], p[i][5]), pack_bf16x2(p[i][6], p[i][7]));
+            for (int i = 0; i < NT; ++i) {
+                float w[8];  // (int8: times the V scale)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = I8 ? p[i][e] * v_scale : p[i][e];
+                pb[i] = make_uint4(pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]),
+                                   pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7]));
+            }
             if (!I8 && grp_b) __syncthreads();  // group B's stage barrier
             // row sums: of the bf16 probabilities by an all-ones A operand, or
             // the lane's part by vector adds
@@ -1794,9 +1798,6 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             for (int i = 0; i < NT; ++i) {
                 if constexpr (kMfmaSum)
                     l_i[i] = mfma16x16x32(ones, pb[i], l_i[i]);
-                else if constexpr (I8)
-                    ls[i] = fmaf(((p[i][0] + p[i][1]) + (p[i][2] + p[i][3])) +
-                                     ((p[i][4] + p[i][5]) + (p[i][6] + p[i][7])), v_inv, ls[i]);
                 else
                     ls[i] += ((p[i][0] + p[i][1]) + (p[i][2] + p[i][3])) +
                              ((p[i][4] + p[i][5]) + (p[i][6] + p[i][7]));
@@ -1904,7 +1905,6 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                     }
                     k_scale *= q_sc[i];
                 }
-                const float v_log = I8 ? __builtin_amdgcn_logf(v_scale) : 0.f;
                 float sc[8], p[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -1932,25 +1932,24 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
 #pragma unroll
                     for (int dt = 0; dt < NT16; ++dt) acc[i][dt] *= alpha;
                 }
+                float w[8];  // (int8: times the V scale)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     if constexpr (I8) {
-                        p[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], k_scale, v_log - m_ref[i]));
                         // (an unseen block's scales may be NaN)
-                        p[e] = lkey0 + e >= vlo && lkey0 + e < vhi ? p[e] : 0.f;
+                        const bool seen = lkey0 + e >= vlo && lkey0 + e < vhi;
+                        p[e] = seen ? __builtin_amdgcn_exp2f(fmaf(sc[e], k_scale, -m_ref[i])) : 0.f;
+                        w[e] = seen ? p[e] * v_scale : 0.f;
                     } else {
                         p[e] = __builtin_amdgcn_exp2f(kShift ? sc[e] : sc[e] - m_ref[i]);
+                        w[e] = p[e];
                     }
                 }
-                const uint4 pb = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]),
-                                            pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+                const uint4 pb = make_uint4(pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]),
+                                            pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7]));
                 if constexpr (kMfmaSum)
                     l_i[i] = mfma16x16x32(make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u),
                                           pb, l_i[i]);
-                else if constexpr (I8)
-                    ls[i] = vlo < vhi ? fmaf(((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])),
-                                             __builtin_amdgcn_exp2f(-v_log), ls[i])
-                                      : ls[i];
                 else
                     ls[i] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
 #pragma nounroll
