@@ -389,7 +389,7 @@ __global__ __launch_bounds__(64 * kI8Waves) void k_attn_i8(I8Args ia) {
                 mx = fmaxf(mx, fabsf(q[s][e]));
             }
         }
-        const int eq = __builtin_amdgcn_frexp_expf(rows_max(mx));  // 0 for zero and for infinities
+        const int eq = min(__builtin_amdgcn_frexp_expf(rows_max(mx)), 127);  // 0 for zero and for infinities
         qscale = ldexpf(1.f, eq);
 #pragma unroll
         for (int s = 0; s < ND; ++s) {

@@ -1380,7 +1380,9 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         }
         // int8: the query in f16 (against exact codes: 11 bits where bf16 has 8), each
         // row scaled by a power of two that its elements' largest magnitude gives;
-        // the rotation adds less than a bit, the form's magnitude few more
+        // the rotation adds less than a bit, the form's magnitude few more.  (The
+        // power and its product with the softmax scale are kept finite, also for the
+        // smallest and largest bf16 queries.)
         float q_sc[kPfTpw];
 #pragma unroll
         for (int i = 0; i < kPfTpw; ++i) {
@@ -1395,7 +1397,8 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(x[e]));
                 }
-                const int eq = max(__builtin_amdgcn_frexp_expf(rows_max(mx) * a.scale_log2) + 1, -100);
+                const int eq = min(max(__builtin_amdgcn_frexp_expf(rows_max(mx) * a.scale_log2) + 1,
+                                       __builtin_amdgcn_frexp_expf(a.scale_log2) - 126), 127);
                 q_sc[i] = ldexpf(1.f, eq);
                 q_mul = ldexpf(a.scale_log2, -eq);
             }

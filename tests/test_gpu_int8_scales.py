@@ -1,5 +1,6 @@
 """GPU tests of the int8 cache with blocks of very different scales: a row's sum
-and log-sum-exp depend on its scores alone, whatever the values' size.
+and log-sum-exp depend on its scores alone, whatever the values' size, and
+scores on the product of a query's and a block's size.
 
 A power of two on the rows of a block moves its scale by that power and leaves
 its codes, so most of what follows is exact.  Where fp32 or bf16 operands
@@ -10,6 +11,7 @@ at most 300 keys and before the division by a sum of at least 1.
 import pytest
 import torch
 
+import paper_2607_02640_amd as mtn
 from tests.test_gpu_int8 import _attend, _plain_pool
 
 pytestmark = pytest.mark.gpu
@@ -109,3 +111,62 @@ def test_a_bad_value_leaves_the_sums(bad, d):
         out, lse = _run(pool, q, k, vs)
         assert (lse - lse1).abs().max() <= 2.5e-5
         assert not torch.isfinite(out[290:, 4:, 3]).any() and torch.isfinite(out[:, :4]).all()
+
+
+def _scaled_pool(d, softmax_scale):
+    kw = dict(n_layers=1, n_q_heads=8, n_kv_heads=2, head_dim=d, n_sink=0, window=None, max_chunk=64,
+              max_sessions=2, n_blocks=40, dtype="int8", max_len=320)
+    kv = torch.empty(mtn.Pool.required(**kw), dtype=torch.uint8, device="cuda")
+    return mtn.Pool(**kw, softmax_scale=softmax_scale, kv=kv)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("scale", [0.0, 1.0])
+@pytest.mark.parametrize("power", [-120, -110, -60, 60, 100, 125])
+def test_small_queries_over_large_keys_and_the_reverse(power, scale, d):
+    """Queries times 2^power over keys times 2^-power: the same scores.  (Where a
+    rotated element is subnormal in fp32 it may round to another bf16 value, which
+    moves a key by a step of its block, 0.035 of the largest, and a score by
+    0.035 * 4.5 * the softmax scale.)"""
+    q, k, v = _rows(d, 3)
+    if scale:
+        q = (q.float() / 8).bfloat16()
+    out1 = lse1 = None
+    for p in (0, power):
+        ks = (k.float() * 2.0 ** -p).bfloat16()
+        out, lse = _run(_scaled_pool(d, scale), (q.float() * 2.0 ** p).bfloat16(), ks, v)
+        if out1 is None:
+            out1, lse1 = out, lse
+    step = 0.035 * 4.5 * (scale / 8 if scale else d ** -0.5)
+    assert (lse - lse1).abs().max() <= step
+    assert (out - out1).abs().max() <= 2 * step * 2 * 4.5 / 4 + 2.0 ** -7 * 4.5
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("pq,pk", [(-84, -84), (-130, -20), (-20, -130), (-133, -133)])
+def test_scores_too_small_to_matter(pq, pk, d):
+    """Every key that a row sees has the same weight, and masked keys none: the
+    log-sum-exp is ln n, the output the mean (to half a step of a code, 0.018, and
+    three bf16 roundings of at most 4.5)."""
+    q, k, v = _rows(d, 4)
+    q, k = (q.float() * 2.0 ** pq).bfloat16(), (k.float() * 2.0 ** pk).bfloat16()
+    out, lse = _run(_plain_pool(d), q, k, v)
+    n = torch.arange(1, 299, device="cuda").double()
+    vf = torch.cat([v, v[-1:]]).double().repeat_interleave(4, 1)
+    assert (lse - n.log()[:, None]).abs().max() <= 2.5e-5
+    assert (out - vf.cumsum(0) / n[:, None, None]).abs().max() <= 0.018 + 3 * 2.0 ** -8 * 4.5
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_near_the_largest_float_over_zero_keys(d):
+    """Scaled and rotated elements of up to 1.5 * 2^126 * log2(e) * sqrt(2) = 1.53 *
+    2^127: finite, so that their scores over zero keys are 0 and every key has the
+    same weight (tolerances as above)."""
+    _, k, v = _rows(d, 5)
+    q = torch.zeros((len(k), 8, d), dtype=torch.bfloat16, device="cuda")
+    q[:, :, [3, 3 + d // 2]] = 1.5 * 2.0 ** 126
+    out, lse = _run(_scaled_pool(d, 1.0), q, torch.zeros_like(k), v)
+    n = torch.arange(1, 299, device="cuda").double()
+    vf = torch.cat([v, v[-1:]]).double().repeat_interleave(4, 1)
+    assert (lse - n.log()[:, None]).abs().max() <= 2.5e-5
+    assert (out - vf.cumsum(0) / n[:, None, None]).abs().max() <= 0.018 + 3 * 2.0 ** -8 * 4.5
