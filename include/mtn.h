@@ -233,8 +233,9 @@ mtn_status mtn_session_close(mtn_pool *pool, int32_t sid);
  * copy after copy, in order of logical block.  Windowed pools reserve each
  * copy's whole footprint as mtn_session_open does.  Errors:
  * MTN_ERR_BAD_SESSION, MTN_ERR_NO_SESSION_SLOT, MTN_ERR_POOL_EXHAUSTED,
- * MTN_ERR_BAD_STATE while a plan is open or the stream is being captured,
- * MTN_ERR_DEVICE.  The next plan may use another stream, as after a plan.
+ * MTN_ERR_BAD_STATE while a plan is open or the stream, or the previous plan's, is
+ * being captured, MTN_ERR_DEVICE.  The next plan may use another stream, as after a
+ * plan.
  */
 mtn_status mtn_session_fork(mtn_pool *pool, int32_t sid, int32_t n_copies, int32_t *sids_out /*host*/,
                             void *stream);
@@ -246,10 +247,11 @@ mtn_status mtn_session_fork(mtn_pool *pool, int32_t sid, int32_t n_copies, int32
  * page is copied on `stream`; the pages take blocks 0, 1, ... of the new buffer in
  * order of session id and logical block, the rest of it is left as it is and
  * free.  Lengths, session ids and results do not change.  The old buffer is the
- * caller's again once the work issued on `stream` so far is done.
+ * caller's again once the work issued on `stream` so far is done; a graph that
+ * captured calls of the pool reads the old one and has to be captured again.
  * MTN_ERR_POOL_EXHAUSTED if the sessions hold or (windowed) have reserved more
- * than n_blocks, MTN_ERR_BAD_STATE while a plan is open or the stream is being
- * captured.  Host-only pools: kv_dev may be NULL.
+ * than n_blocks, MTN_ERR_BAD_STATE while a plan is open or the stream, or the
+ * previous plan's, is being captured.  Host-only pools: kv_dev may be NULL.
  */
 mtn_status mtn_pool_resize(mtn_pool *pool, int64_t n_blocks, void *kv_dev, size_t kv_bytes,
                            void *stream);

@@ -551,14 +551,18 @@ mtn_status follow_last_stream(mtn_pool *P, void *stream) {
 }
 
 // Page operations change the host's tables as they are called, so a captured
-// one could not be replayed.
+// one could not be replayed; and work that follows a capturing stream would
+// join its capture.
 mtn_status refuse_capture(mtn_pool *P, void *stream) {
     if (P->host_only) return MTN_OK;
-    hipStreamCaptureStatus c = hipStreamCaptureStatusNone;
-    const hipError_t e = hipStreamIsCapturing((hipStream_t)stream, &c);
-    if (e == hipSuccess && c == hipStreamCaptureStatusNone) return MTN_OK;
-    (void)hipGetLastError();
-    return fail(P, MTN_ERR_BAD_STATE, "page operations cannot be captured");
+    for (void *s : {stream, P->have_last_stream ? P->last_stream : stream}) {
+        hipStreamCaptureStatus c = hipStreamCaptureStatusNone;
+        const hipError_t e = hipStreamIsCapturing((hipStream_t)s, &c);
+        if (e == hipSuccess && c == hipStreamCaptureStatusNone) continue;
+        (void)hipGetLastError();
+        return fail(P, MTN_ERR_BAD_STATE, "the stream, or the previous plan's, is being captured");
+    }
+    return MTN_OK;
 }
 
 // Sink blocks among a session's assigned ones.  Slots fill from the first on,
