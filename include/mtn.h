@@ -209,8 +209,10 @@ typedef struct {
     double  magnitude;     /* 0 = by scaling, else up to 1024                  */
 } mtn_rope_config;
 
-/* Synchronises the stream of the pool's previous plan.  An all-zero config is
- * the form that a pool is created with.                                       */
+/* Synchronises the stream of the pool's previous plan; MTN_ERR_BAD_STATE while
+ * that stream is being captured.  The call takes effect at once and is part of no
+ * graph: one that captured calls of the pool keeps the form of its capture and has
+ * to be captured again.  An all-zero config is the form that a pool is created with. */
 mtn_status mtn_pool_set_rope(mtn_pool *pool, const mtn_rope_config *rope);
 
 /* Open a session: lowest free session id.  Windowed pools reserve the

@@ -320,6 +320,10 @@ class Pool:
                  beta_fast=0.0, beta_slow=0.0, magnitude=0.0) -> None:
         """Rotary positions of later appends and queries (mtn_pool_set_rope): layout
         "half" or "interleaved", scaling "none", "linear", "base" or "yarn"."""
+        if not self.host_only:
+            import torch
+            if torch.cuda.is_current_stream_capturing():
+                raise MtnError(MTN_ERR_BAD_STATE, "set_rope", "the current stream is being captured")
         cfg = RopeConfig(ROPE_LAYOUTS[layout], rotary_dim, ROPE_SCALINGS[scaling], original_len,
                          factor, beta_fast, beta_slow, magnitude)
         self._check(self.lib.mtn_pool_set_rope(self.h, C.byref(cfg)), "set_rope")

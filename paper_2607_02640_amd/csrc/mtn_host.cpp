@@ -550,9 +550,9 @@ mtn_status follow_last_stream(mtn_pool *P, void *stream) {
     return MTN_OK;
 }
 
-// Page operations change the host's tables as they are called, so a captured
-// one could not be replayed; and work that follows a capturing stream would
-// join its capture.
+// Page operations and the rotary form change the host's state as they are
+// called, so a captured one could not be replayed; and work that follows a
+// capturing stream would join its capture.
 mtn_status refuse_capture(mtn_pool *P, void *stream) {
     if (P->host_only) return MTN_OK;
     for (void *s : {stream, P->have_last_stream ? P->last_stream : stream}) {
@@ -1440,9 +1440,17 @@ mtn_status mtn_pool_set_rope(mtn_pool *P, const mtn_rope_config *rope) {
         if (st) return fail(P, st, "bad rotary config");
         const std::vector<double> t = rope_table(P->cfg, *rope);
         if (!P->host_only) {
-            // plans of closed sessions may still read the table
-            if (P->have_last_stream) HIP_TRY(P, hipStreamSynchronize((hipStream_t)P->last_stream));
-            HIP_TRY(P, hipMemcpy(P->d_inv_freq, t.data(), sizeof(double) * t.size(), hipMemcpyHostToDevice));
+            // On the previous plan's stream: plans of closed sessions may still read
+            // the table.  A capture under way on some other stream is left alone.
+            void *const last = P->have_last_stream ? P->last_stream : nullptr;
+            if (mtn_status cs = refuse_capture(P, last)) return cs;
+            hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+            HIP_TRY(P, hipThreadExchangeStreamCaptureMode(&mode));
+            hipError_t e = hipMemcpyAsync(P->d_inv_freq, t.data(), sizeof(double) * t.size(),
+                                          hipMemcpyHostToDevice, (hipStream_t)last);
+            if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)last);
+            (void)hipThreadExchangeStreamCaptureMode(&mode);
+            if (e != hipSuccess) return hip_fail(P, e, "rotary table");
         }
         P->rope_half = (rope->rotary_dim ? rope->rotary_dim : P->cfg.head_dim) / 2;
         P->rope_il = rope->layout == MTN_ROPE_INTERLEAVED;
