@@ -983,7 +983,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
     constexpr int ND = D / 32;   // 32-wide slices of d (QK MFMAs per key row)
     constexpr int NT16 = D / 16; // 16-wide tiles of d (PV MFMAs)
     constexpr int SB = F8 ? 2 * kF8Read : I8 ? 2 * kI8Blk : Lds::kStage;  // bytes of a ring stage
-    static_assert(kPfStages >= 3 && kPfStages <= 8, "ring depth (the DMA waits count at most 63)");
+    static_assert(kPfStages <= 8, "ring depth (the DMA waits count at most 63)");
     static_assert(kPfEarly >= 1 && kPfEarly <= kPfStages - 1, "early stages are ring prologue stages");
     __shared__ __attribute__((aligned(16))) uint8_t ring[kPfStages][SB];
     __shared__ __attribute__((aligned(16))) uint8_t bfs[I8 ? 4 : F8 ? 2 : 1][Q8 ? Lds::kStage : 16];
@@ -1618,6 +1618,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         // (five registers spilled), 309 converting one stage ahead, 305 with the
         // conversion between the MFMAs, 279 with the groups apart.
         constexpr int kAhead = I8 ? 2 : kPP ? 1 : 0;  // stages that land further ahead
+        static_assert(kPfStages >= 3 + kAhead, "ring depth (the stage's wait leaves kPfStages - 3 - kAhead stages)");
         if (dma_wave) vm_wait<NPW * (kPfStages - 2 - kAhead)>();  // stage 0 (and 1) landed
         __syncthreads();
         if constexpr (Q8) {
