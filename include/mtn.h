@@ -465,9 +465,10 @@ mtn_status mtn_pool_last_split(const mtn_pool *pool, int32_t *n_split);
 
 /* Test hook: the launch point with index launch_index (0 = the next one)
  * among this pool's later append / prefill / decode launch points fails with
- * MTN_ERR_DEVICE before launching; -1 disarms.  Host-only pools pass through
- * the same points inside mtn_frame_step, so error paths can be exercised on a
- * host without a GPU.                                                        */
+ * MTN_ERR_DEVICE before launching; -1 disarms.  mtn_session_fork and
+ * mtn_pool_resize have one before their first work and one at each launch.
+ * Host-only pools pass through the same points inside mtn_frame_step and these
+ * two, so error paths can be exercised on a host without a GPU.              */
 mtn_status mtn_debug_inject_failure(mtn_pool *pool, int64_t launch_index);
 
 /* Per-kernel device timing.  When enabled, the library records HIP events

@@ -303,7 +303,7 @@ inline void logical_slot(const mtn_pool *P, int64_t p, int32_t *lb, int32_t *off
 }
 
 TailView tails(const mtn_pool *P) {
-    return P->int8 ? TailView{P->kv + tails_offset(&P->cfg), tail_stride(&P->cfg)} : TailView{nullptr, 0};
+    return P->int8 && P->kv ? TailView{P->kv + tails_offset(&P->cfg), tail_stride(&P->cfg)} : TailView{nullptr, 0};
 }
 // int8: rows of a session's open block (0 where its last block is complete)
 int32_t open_rows(const mtn_pool *P, int64_t len) {
@@ -587,7 +587,8 @@ mtn_status copy_tails(mtn_pool *P, const TailView &from, const TailView &to,
             a.src[j] = slots[i + j].first;
             a.dst[j] = slots[i + j].second;
         }
-        HIP_TRY(P, launch_copy_tails(a, s));
+        if (mtn_status st = launch_gate(P)) return st;
+        if (!P->host_only) HIP_TRY(P, launch_copy_tails(a, s));
     }
     return MTN_OK;
 }
@@ -615,7 +616,8 @@ mtn_status fork_pages(mtn_pool *P, int32_t src, const std::vector<int32_t> &sids
                 for (int32_t i = 0; i < a.m; ++i)
                     a.block[c * a.m + i] =
                         P->table[(size_t)a.sid[c] * P->row_len + page_lb(P, src, a.first + i)];
-            HIP_TRY(P, launch_fork(a, P->cfg.n_layers, s));
+            if (mtn_status st = launch_gate(P)) return st;
+            if (!P->host_only) HIP_TRY(P, launch_fork(a, P->cfg.n_layers, s));
         }
     }
     return copy_tails(P, tails(P), tails(P), tail_slots, s);
@@ -1541,7 +1543,7 @@ mtn_status mtn_session_fork(mtn_pool *P, int32_t sid, int32_t n_copies, int32_t 
             int32_t *row = &P->table[(size_t)c * P->row_len];
             for (int32_t i = 0; i < pages; ++i) row[page_lb(P, sid, i)] = (int32_t)P->alloc.take();
         }
-        if (!P->host_only && pages) {
+        if (pages) {
             st = fork_pages(P, sid, sids, tail_slots, (hipStream_t)stream);
             if (st) {  // the blocks go back; what a launch wrote lies in free blocks
                 for (const int32_t c : sids) {
@@ -1605,7 +1607,7 @@ mtn_status mtn_pool_resize(mtn_pool *P, int64_t n_blocks, void *kv_dev, size_t k
         if (!st) st = follow_last_stream(P, stream);
         if (st) return st;
         const int64_t layer_stride = P->block_stride * n_blocks;
-        if (!P->host_only && !moves.empty()) {
+        if (!moves.empty()) {
             MoveArgs a;
             a.kv = P->kv;
             a.to = (uint8_t *)kv_dev;
@@ -1615,31 +1617,34 @@ mtn_status mtn_pool_resize(mtn_pool *P, int64_t n_blocks, void *kv_dev, size_t k
             a.table = P->d_table;
             a.row_len = P->row_len;
             a.n_sink_blocks = P->nsb;
-            auto each = [&](auto &&launch) {
-                hipError_t e = hipSuccess;
-                for (size_t i = 0; i < moves.size() && e == hipSuccess; i += kMoveSessions) {
+            auto each = [&](auto &&launch) -> mtn_status {
+                for (size_t i = 0; i < moves.size(); i += kMoveSessions) {
                     a.n = (int32_t)std::min<size_t>(kMoveSessions, moves.size() - i);
                     std::copy_n(&moves[i], a.n, a.s);
-                    e = launch();
+                    if (mtn_status g = launch_gate(P)) return g;
+                    if (!P->host_only) HIP_TRY(P, launch());
                 }
-                return e;
+                return MTN_OK;
             };
-            HIP_TRY(P, each([&] { return launch_move(a, P->cfg.n_layers, (hipStream_t)stream); }));
+            st = each([&] { return launch_move(a, P->cfg.n_layers, (hipStream_t)stream); });
+            if (st) return st;
             if (P->int8) {
                 std::vector<std::pair<int32_t, int32_t>> slots;
                 for (const MoveSession &m : moves)
                     if (open_rows(P, P->len[m.sid]))
                         slots.emplace_back(2 * m.sid + P->tail[m.sid], 2 * m.sid + P->tail[m.sid]);
-                const TailView to{(uint8_t *)kv_dev + tails_offset(&cfg), tail_stride(&cfg)};
+                const TailView to{kv_dev ? (uint8_t *)kv_dev + tails_offset(&cfg) : nullptr, tail_stride(&cfg)};
                 st = copy_tails(P, tails(P), to, slots, (hipStream_t)stream);
                 if (st) return st;
             }
-            const hipError_t e = each([&] { return launch_move_table(a, (hipStream_t)stream); });
-            if (e != hipSuccess) {  // back to the tables of the old buffer
-                (void)hipStreamSynchronize((hipStream_t)stream);
-                (void)hipMemcpy(P->d_table, P->table.data(), sizeof(int32_t) * P->table.size(),
-                                hipMemcpyHostToDevice);
-                return hip_fail(P, e, "launch_move_table");
+            st = each([&] { return launch_move_table(a, (hipStream_t)stream); });
+            if (st) {  // back to the tables of the old buffer
+                if (!P->host_only) {
+                    (void)hipStreamSynchronize((hipStream_t)stream);
+                    (void)hipMemcpy(P->d_table, P->table.data(), sizeof(int32_t) * P->table.size(),
+                                    hipMemcpyHostToDevice);
+                }
+                return st;
             }
         }
         for (const MoveSession &m : moves)
