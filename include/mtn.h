@@ -180,7 +180,8 @@ void mtn_pool_destroy(mtn_pool *pool);
  * (angle in fp64) and scaled by m:
  *   y_a = m (x_a cos - x_b sin),   y_b = m (x_b cos + x_a sin)
  * where (a, b) is (i, i + rd/2) for MTN_ROPE_HALF and (2i, 2i + 1) for
- * MTN_ROPE_INTERLEAVED; elements rd .. D - 1 are left as they are.
+ * MTN_ROPE_INTERLEAVED; elements rd .. D - 1 are left as they are (multiplied by
+ * (cos, sin) = (1, 0) in pairs as well: an infinite one makes the other NaN).
  *   NONE    f_i = theta^(-2i/rd)
  *   LINEAR  f_i = theta^(-2i/rd) / factor              (positions divided)
  *   BASE    theta replaced by theta * factor^(rd/(rd-2))
@@ -319,7 +320,8 @@ mtn_status mtn_frame_append_kv(mtn_pool *pool, int32_t layer, const void *k, con
  * position t is rotated at t and attends to sinks [0, min(S, t+1)) and window
  * [max(S, t-W+1), t] of its own session (all earlier chunk tokens included).
  * lse: device [T][Hq] fp32 natural-log sum-exp of the scaled scores, or NULL.
- * bf16 and 8-bit pools run the bf16 MFMA kernel, fp32 pools an fp32 MFMA kernel.
+ * bf16 and 8-bit pools run one MFMA kernel over bf16 operands (int8: the scores'
+ * product over f16 ones), fp32 pools an fp32 MFMA kernel.
  */
 mtn_status mtn_attend_chunk_prefill(mtn_pool *pool, int32_t layer, const void *q, void *out,
                                     float *lse, void *stream);

@@ -416,6 +416,11 @@ int64_t keys_seen(const mtn_pool *P, int64_t t0, int64_t t1) {
 // stage (two blocks; fp32: one), with `rpp` query rows per pass (fp32: 64); and
 // those that cutting the passes into segments adds: the merge's launch, its one
 // wave per output row, and the partial rows written and read (see plan_prefill).
+// The int8 instance has no fit of its own: with these figures (FP8's at D = 128,
+// bf16's at 64) its choices are within 11 % of the best of eight segment counts and
+// both pass sizes in 19 of 20 shapes of 1 to 24 sessions, 10 to 200 tokens, 400 to
+// 4100 keys (median 4 %; 16 sessions over 404 keys at G = 8, D = 128 29.4 us with 256
+// rows, 24.0 with 128).
 struct PfCost {
     double start, stage;
 };
@@ -1385,7 +1390,13 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
         if (fp8)
             P->resident_mfma = n_cu * attn_fp8_resident_per_cu(P->G);
         else if (P->int8)
-            P->resident_mfma = n_cu;  // one workgroup each (see k_attn_i8's copies ahead)
+            // One workgroup each (see k_attn_i8's copies ahead).  Per launch with the merge,
+            // G = 8, D = 128, 4100 keys, 1 to 63 sessions, against 1, 2, 3, 4, 6, 8, 16 and 32
+            // segments: the best to 2.4 %, but 24 sessions 34.4 us in two, 32.4 in eight, 40
+            // 46.0 unsplit, 41.7 in three (G = 4: the same).  D = 64, G = 8: up to 24 sessions
+            // the best to 4 %, then more would be: 32 sessions 21.9 us in four, 19.8 in
+            // eight, 48 29.3 in two, 22.9 in eight, 63 29.5 in two, 25.2 in four.
+            P->resident_mfma = n_cu;
         else if (cfg->kv_dtype == MTN_BF16 && attn_mfma_bf16_supported(cfg->head_dim, P->G))
             P->resident_mfma = n_cu * attn_mfma_bf16_resident_per_cu(cfg->head_dim, P->G);
         if (!fp8 && !P->int8)

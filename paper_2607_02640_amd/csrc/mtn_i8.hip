@@ -229,9 +229,11 @@ __global__ __launch_bounds__(256) void k_append_i8(PoolGeom g, PlanView p, int32
 // the tail, or, where they complete the block, quantizes the block, uses and
 // stores it.
 //
-// Bound by the stream of codes (5.8 TB/s at 128 sessions of G = 8, 4100 keys: 94 us
-// a launch, the FP8 kernel 89).  Per block a wave converts 4096 codes in 80 vector
-// instructions (K 32, V 48), against 32 of the FP8 kernel.
+// Bound by the stream of codes (5.8 TB/s at 128 sessions of G = 8, 4100 keys: 93 to
+// 95 us a launch, the FP8 kernel 89; D = 64, 128 sessions of G = 8, 256 units, 38.7
+// us, 3.5 TB/s: a CU's one workgroup waits for copies of 2 KiB; 256 sessions 52.8,
+// 5.1 TB/s).  Per block a wave converts 4096 codes in 80 vector instructions (K 32, V
+// 48), against 32 of the FP8 kernel.
 // Launch shape: four waves a workgroup with two-block rings at every group size.
 // (Eight waves, which the FP8 kernel takes below G = 8: 8 KV heads, G = 4, 60
 // sessions of 2048 keys 50.3 us against 48.9, 32 sessions 32.1 against 29.7; 200

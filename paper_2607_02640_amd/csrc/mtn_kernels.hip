@@ -1614,9 +1614,10 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         // bf16 buffers, beside the PV MFMAs of the iteration's own stage: one barrier
         // a stage, met by the two groups of waves as by bf16's, and V read only
         // once the K fragments' registers are free.  128 sessions of G = 8, 25 tokens,
-        // per layer: 343 us with the FP8 kernel's two buffers and two barriers
-        // (five registers spilled), 309 converting one stage ahead, 305 with the
-        // conversion between the MFMAs, 279 with the groups apart.
+        // per layer, step by step: 343 us with the FP8 kernel's two buffers and two
+        // barriers (five registers spilled), 309 converting one stage ahead, 305 with
+        // the conversion between the MFMAs, 279 with the groups apart.  (Now 281 to 290
+        // on four boxes, with V converted in whole chunks and the V scale out of the sums.)
         constexpr int kAhead = I8 ? 2 : kPP ? 1 : 0;  // stages that land further ahead
         static_assert(kPfStages >= 3 + kAhead, "ring depth (the stage's wait leaves kPfStages - 3 - kAhead stages)");
         if (dma_wave) vm_wait<NPW * (kPfStages - 2 - kAhead)>();  // stage 0 (and 1) landed
