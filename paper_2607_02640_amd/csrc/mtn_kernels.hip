@@ -1617,7 +1617,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         // per layer, step by step: 343 us with the FP8 kernel's two buffers and two
         // barriers (five registers spilled), 309 converting one stage ahead, 305 with
         // the conversion between the MFMAs, 279 with the groups apart.  (Now 281 to 290
-        // on four boxes, with V converted in whole chunks and the V scale out of the sums.)
+        // in four runs, with V converted in whole chunks and the V scale out of the sums.)
         constexpr int kAhead = I8 ? 2 : kPP ? 1 : 0;  // stages that land further ahead
         static_assert(kPfStages >= 3 + kAhead, "ring depth (the stage's wait leaves kPfStages - 3 - kAhead stages)");
         if (dma_wave) vm_wait<NPW * (kPfStages - 2 - kAhead)>();  // stage 0 (and 1) landed
