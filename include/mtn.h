@@ -216,6 +216,29 @@ typedef struct {
  * to be captured again.  An all-zero config is the form that a pool is created with. */
 mtn_status mtn_pool_set_rope(mtn_pool *pool, const mtn_rope_config *rope);
 
+/*
+ * Norms of queries and keys.  A pool is created without; after
+ * mtn_pool_set_qk_norm every row of D elements of q and k that a later call
+ * brings is normed before it is rotated, in the pass that rotates it:
+ *   y_d = x_d * w_d / sqrt((x_0^2 + .. + x_{D-1}^2) / D + eps)
+ * over each token and head, with the query's or the key's weights of the layer, in
+ * fp32 (the sum is scaled where it would overflow: any row of finite elements is
+ * normed), and rounded once, after the rotation, as without a norm.  The pool then holds
+ * normed, rotated keys.  Values are left as they are.  Weights are in the order of
+ * the input row's elements, whatever the rotary form.
+ */
+typedef struct {
+    const float *q_weight; /* host [n_layers][head_dim], finite; NULL = all ones */
+    const float *k_weight; /* ... for keys                                       */
+    double       eps;      /* 2^-126 <= eps <= 1                                 */
+} mtn_qk_norm_config;
+
+/* NULL takes the norms away again.  While no open session holds tokens and no plan
+ * is open (MTN_ERR_BAD_STATE otherwise); synchronises and refuses a capture as
+ * mtn_pool_set_rope does, and captured calls keep whether they norm, but read the
+ * weights that are set when they are replayed.  The weights are copied. */
+mtn_status mtn_pool_set_qk_norm(mtn_pool *pool, const mtn_qk_norm_config *norm);
+
 /* Open a session: lowest free session id.  Windowed pools reserve the
  * session's whole bounded footprint, ceil(S/16) sink blocks plus R/16 ring
  * blocks with R = roundup(W + max_chunk - 1, 16), and fail with
@@ -302,7 +325,8 @@ mtn_status mtn_plan_abort(mtn_pool *pool);
  * the absolute position they were appended at; App. A: positions behind the
  * window are not retained, sink blocks stay).
  * k, v: device, [T][Hkv][D] in kv_dtype, T = total planned tokens, packed in
- * plan order.  Each key row is rotated (RoPE at its absolute position,
+ * plan order.  Each key row is normed where mtn_pool_set_qk_norm says so,
+ * rotated (RoPE at its absolute position,
  * rotate-half unless mtn_pool_set_rope says otherwise, angle computed in fp64) and written with its value into the
  * token's slot of layer `layer`, overwriting whatever position left the window
  * there (eviction is slot reuse).  Errors: MTN_ERR_BAD_STATE (no open plan,
@@ -317,7 +341,7 @@ mtn_status mtn_frame_append_kv(mtn_pool *pool, int32_t layer, const void *k, con
  * the frame's chunk attends causally inside itself and to the retained cache
  * (§2, the task model; §4.1 and App. A for the per-query mask).
  * q, out: device, [T][Hq][D], packed like k/v.  Each planned query row at
- * position t is rotated at t and attends to sinks [0, min(S, t+1)) and window
+ * position t is normed (where set), rotated at t and attends to sinks [0, min(S, t+1)) and window
  * [max(S, t-W+1), t] of its own session (all earlier chunk tokens included).
  * lse: device [T][Hq] fp32 natural-log sum-exp of the scaled scores, or NULL.
  * bf16 and 8-bit pools run one MFMA kernel over bf16 operands (int8: the scores'

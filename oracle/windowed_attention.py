@@ -171,6 +171,12 @@ def rope_form(x: np.ndarray, pos: int, theta: float, *, layout: str = "half",
     return y
 
 
+def rms_norm(x: np.ndarray, weight: np.ndarray, eps: float) -> np.ndarray:
+    """Rows x[..., D] over their root mean square, times a weight per element."""
+    x = np.asarray(x, dtype=np.float64)
+    return x / np.sqrt(np.mean(x * x, axis=-1, keepdims=True) + eps) * np.asarray(weight, np.float64)
+
+
 # ---------------------------------------------------------------------------
 # One query row against an explicit key set
 # ---------------------------------------------------------------------------
@@ -216,6 +222,8 @@ class OracleSession:
         self.window = window
         self.theta = theta
         self.rope = rope  # rope_form's keywords, or None for whole rotate-half rows
+        # (query weights [n_layers, D], key weights, eps), or None: rows are only rotated
+        self.qk_norm = None
         self.scale = 1.0 / math.sqrt(head_dim) if scale is None else scale
         self.n_layers = n_layers
         self.literal = literal_window
@@ -237,6 +245,11 @@ class OracleSession:
         if self.rope is None:
             return rope_rotate(x, pos, self.theta)
         return rope_form(x, pos, self.theta, **self.rope)
+
+    def _normed(self, x: np.ndarray, layer: int, key: bool) -> np.ndarray:
+        if self.qk_norm is None:
+            return x
+        return rms_norm(x, self.qk_norm[1 if key else 0][layer], self.qk_norm[2])
 
     # -- frame structure -------------------------------------------------
     def begin(self, n_tok: int) -> List[int]:
@@ -266,7 +279,7 @@ class OracleSession:
         # Insert every chunk token first: each query then sees the earlier
         # tokens of its own chunk (causal inside the chunk).
         for i in range(c):
-            kr = self._rotate(k[i], base + i)
+            kr = self._rotate(self._normed(k[i], layer, True), base + i)
             vi = v[i].copy()
             if self.kv_quant == "fp8_e4m3":
                 # the cache holds what the quantized pool returns: each
@@ -292,7 +305,7 @@ class OracleSession:
             assert not missing, f"visible positions not resident: {missing[:5]}"
             kmat = np.stack([st[p][0] for p in vis])  # [n, Hkv, D]
             vmat = np.stack([st[p][1] for p in vis])
-            qr = self._rotate(q[i], t)                # [Hq, D]
+            qr = self._rotate(self._normed(q[i], layer, False), t)  # [Hq, D]
             for h in range(self.hq):
                 kv = h // self.g
                 o, l, psum = attend_row(qr[h], kmat[:, kv, :], vmat[:, kv, :],

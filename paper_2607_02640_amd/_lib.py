@@ -46,7 +46,7 @@ EXPORTS = [
     "mtn_pool_required_bytes", "mtn_pool_create", "mtn_pool_destroy",
     "mtn_session_open", "mtn_session_close", "mtn_plan_begin", "mtn_plan_commit",
     "mtn_plan_abort",
-    "mtn_pool_set_rope", "mtn_session_fork", "mtn_pool_resize",
+    "mtn_pool_set_rope", "mtn_pool_set_qk_norm", "mtn_session_fork", "mtn_pool_resize",
     "mtn_frame_append_kv", "mtn_attend_chunk_prefill", "mtn_attend_decode",
     "mtn_attend_decode_append", "mtn_attend_decode_noalloc",
     "mtn_frame_step", "mtn_pool_stats", "mtn_session_info", "mtn_session_block_table",
@@ -75,6 +75,10 @@ class RopeConfig(C.Structure):
         ("original_len", C.c_int32), ("factor", C.c_double), ("beta_fast", C.c_double),
         ("beta_slow", C.c_double), ("magnitude", C.c_double),
     ]
+
+
+class QkNormConfig(C.Structure):
+    _fields_ = [("q_weight", C.POINTER(C.c_float)), ("k_weight", C.POINTER(C.c_float)), ("eps", C.c_double)]
 
 
 class PoolStats(C.Structure):
@@ -134,6 +138,7 @@ def load() -> C.CDLL:
         "mtn_pool_create": (i32, [C.POINTER(PoolConfig), vp, C.c_size_t, vp, C.POINTER(vp)]),
         "mtn_pool_destroy": (None, [vp]),
         "mtn_pool_set_rope": (i32, [vp, C.POINTER(RopeConfig)]),
+        "mtn_pool_set_qk_norm": (i32, [vp, C.POINTER(QkNormConfig)]),
         "mtn_session_fork": (i32, [vp, i32, i32, P32, vp]),
         "mtn_pool_resize": (i32, [vp, i64, vp, C.c_size_t, vp]),
         "mtn_session_open": (i32, [vp, P32]),
@@ -188,6 +193,18 @@ class MtnError(RuntimeError):
 
 def _arr32(xs: Sequence[int]):
     return (C.c_int32 * len(xs))(*[int(x) for x in xs])
+
+
+def _host_floats(x, where: str, n: int):
+    """``n`` host floats of a tensor, array or nested list, or None (NULL)."""
+    if x is None:
+        return None
+    import numpy as np
+    a = x.detach().to("cpu").float().numpy() if hasattr(x, "detach") else x
+    a = np.ascontiguousarray(a, dtype=np.float32).reshape(-1)
+    if a.size != n:
+        raise MtnError(MTN_ERR_INVALID_ARG, where, f"{a.size} values instead of {n}")
+    return (C.c_float * n)(*a.tolist())
 
 
 def _ptr(t) -> Optional[int]:
@@ -316,17 +333,35 @@ class Pool:
     def plan_abort(self) -> None:
         self._check(self.lib.mtn_plan_abort(self.h), "plan_abort")
 
+    def _not_captured(self, where: str) -> None:
+        if not self.host_only:
+            import torch
+            if torch.cuda.is_current_stream_capturing():
+                raise MtnError(MTN_ERR_BAD_STATE, where, "the current stream is being captured")
+
     def set_rope(self, *, layout="half", rotary_dim=0, scaling="none", factor=1.0, original_len=0,
                  beta_fast=0.0, beta_slow=0.0, magnitude=0.0) -> None:
         """Rotary positions of later appends and queries (mtn_pool_set_rope): layout
         "half" or "interleaved", scaling "none", "linear", "base" or "yarn"."""
-        if not self.host_only:
-            import torch
-            if torch.cuda.is_current_stream_capturing():
-                raise MtnError(MTN_ERR_BAD_STATE, "set_rope", "the current stream is being captured")
+        self._not_captured("set_rope")
         cfg = RopeConfig(ROPE_LAYOUTS[layout], rotary_dim, ROPE_SCALINGS[scaling], original_len,
                          factor, beta_fast, beta_slow, magnitude)
         self._check(self.lib.mtn_pool_set_rope(self.h, C.byref(cfg)), "set_rope")
+
+    def set_qk_norm(self, q_weight=None, k_weight=None, eps: float = 1e-6) -> None:
+        """Norm every query and key row before it is rotated (mtn_pool_set_qk_norm).
+        Weights: [n_layers][head_dim], a tensor of any device, an array or lists;
+        None is all ones."""
+        self._not_captured("set_qk_norm")
+        n = self.cfg.n_layers * self.cfg.head_dim
+        w = [_host_floats(x, "set_qk_norm", n) for x in (q_weight, k_weight)]
+        cfg = QkNormConfig(*(C.cast(x, C.POINTER(C.c_float)) for x in w), eps)
+        self._check(self.lib.mtn_pool_set_qk_norm(self.h, C.byref(cfg)), "set_qk_norm")
+
+    def clear_qk_norm(self) -> None:
+        """Back to rows that are only rotated."""
+        self._not_captured("clear_qk_norm")
+        self._check(self.lib.mtn_pool_set_qk_norm(self.h, None), "clear_qk_norm")
 
     def set_decode_kernel(self, kind: int) -> None:
         """0 = by shape, 1 = vector kernel, 2 = matrix-core kernel."""

@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
+#include <type_traits>
 
 namespace mtn {
 namespace {
@@ -132,8 +133,9 @@ __device__ __forceinline__ void wave_sync() {
 // ---------------------------------------------------------------------------
 // rotation pairs of an input row (see PoolGeom)
 // ---------------------------------------------------------------------------
-// The kernels that rotate are built twice: RF false for whole rotate-half rows,
-// whose offsets are constants, RF true for every other form.  With one
+// The kernels that rotate are built three times: RF 0 for whole rotate-half rows,
+// whose offsets are constants, 1 for every other form, 2 for pools that norm
+// queries and keys, in any form.  With one
 // instance that tests the form, a lone session's frame of 768 decode
 // launches took 9.76 ms instead of 9.68, two-layer fp32 frames 349 us instead
 // of 340.  Both instances round alike, so that a form's results differ from the
@@ -142,17 +144,33 @@ __device__ __forceinline__ void wave_sync() {
 // N(0, 1) rows are 0.0029 off in rms against 0.0018 with fp32 operands, which is the
 // output's own rounding; a second product for the query's low bits would be half as
 // many MFMAs again).
-inline bool rope_form(const PoolGeom &g) { return g.rope_il || g.rope_half != g.d / 2; }
+inline int rope_form(const PoolGeom &g) {
+    return g.rope_il & kRopeNorm ? 2 : g.rope_il || g.rope_half != g.d / 2;
+}
+// f(form as an integral constant)
+template <class F>
+auto with_form(const PoolGeom &g, F &&f) {
+    switch (rope_form(g)) {
+        case 0: return f(std::integral_constant<int, 0>{});
+        case 1: return f(std::integral_constant<int, 1>{});
+        default: return f(std::integral_constant<int, 2>{});
+    }
+}
+// pairs are neighbouring elements
+template <int RF>
+__device__ __forceinline__ bool rope_il(const PoolGeom &g) {
+    return RF == 2 ? g.rope_il & kRopeInterleaved : g.rope_il != 0;
+}
 // Elements of an input row that become dims i and i + D/2 (i < D/2)
-template <bool RF>
+template <int RF>
 __device__ __forceinline__ int rope_a(const PoolGeom &g, int i) {
     if constexpr (!RF) return i;
-    return g.rope_il ? 2 * i : i < g.rope_half ? i : i + g.rope_half;
+    return rope_il<RF>(g) ? 2 * i : i < g.rope_half ? i : i + g.rope_half;
 }
-template <bool RF>
+template <int RF>
 __device__ __forceinline__ int rope_b(const PoolGeom &g, int i, int D) {
     if constexpr (!RF) return i + D / 2;
-    return g.rope_il ? 2 * i + 1 : i < g.rope_half ? i + g.rope_half : i + D / 2;
+    return rope_il<RF>(g) ? 2 * i + 1 : i < g.rope_half ? i + g.rope_half : i + D / 2;
 }
 // The same for a vector of n dims d0 .. d0 + n - 1 (n divides d0, 8 and
 // rope_half) and its partners: the offsets of two vectors that hold them,
@@ -160,11 +178,11 @@ __device__ __forceinline__ int rope_b(const PoolGeom &g, int i, int D) {
 struct RopeSrc {
     int x, y;
 };
-template <bool RF>
+template <int RF>
 __device__ __forceinline__ RopeSrc rope_src(const PoolGeom &g, int d0, int n, int D) {
     if constexpr (!RF) return RopeSrc{d0, d0 ^ (D / 2)};
     const int i0 = d0 & (D / 2 - 1);
-    if (g.rope_il) return RopeSrc{2 * i0, 2 * i0 + n};
+    if (rope_il<RF>(g)) return RopeSrc{2 * i0, 2 * i0 + n};
     const int a = i0 < g.rope_half ? i0 : i0 + g.rope_half;
     const int b = i0 < g.rope_half ? i0 + g.rope_half : i0 + D / 2;
     return d0 < D / 2 ? RopeSrc{a, b} : RopeSrc{b, a};
@@ -192,6 +210,79 @@ __device__ __forceinline__ void rope_split_f32(uint4 &x, uint4 &y, bool upper) {
     const uint4 ev = make_uint4(u.x, u.z, w.x, w.z), od = make_uint4(u.y, u.w, w.y, w.w);
     x = upper ? od : ev;
     y = upper ? ev : od;
+}
+
+// ---------------------------------------------------------------------------
+// norms of queries and keys (RF 2): x -> x r w before the rotation, with
+// r = 1 / sqrt(mean(x^2) + eps) over the row's D elements
+// ---------------------------------------------------------------------------
+// fp32 throughout, nothing is rounded to fewer bits between norm and rotation.  The
+// rows are in registers where they are rotated, so a norm moves no byte but its
+// weights; it costs the reduction over the lanes that share a row and the products,
+// before the first key is looked at: per launch 1.3 us of a lone session's decode
+// (G = 8, D = 128: 9.7 -> 11.0), 85.4 -> 87.4 us of 128 sessions' over 2052 keys, 133
+// -> 136 of their chunk prefill and 10.5 -> 11.9 of the append, 25.5 -> 29.6 of
+// 13 fp32 sessions' decode at G = 4 (whose lanes rotate every element 16 times).  A sum of
+// squares past 2^120 is taken once more of elements times 2^-70, so that no row of
+// finite elements overflows it.  (In 64 bits, where nothing overflows and bf16
+// squares add without rounding, the append of 128 x 25 tokens of 4 heads took
+// 14.0 us instead of 10.5 without norms; see k_append.)
+//
+// Several kernels store keys (append, decode and prefill with the append fused), and
+// their bytes agree: each adds a key's squares in one order, a tree over the bits
+// of the dim, D/2 first, then 1, 2, 4, .. (row_square: the pair of dims i and i + D/2 of
+// lane i, then the lanes), in ordinary products and sums.
+struct NormView {
+    const float *q, *k;  // weights in the order of the kernels' dims
+    float eps;
+};
+// The library keeps them in front of the rotary table, layer l in the (l + 1)-th
+// place from it: no kernel argument of their own (see PoolGeom).
+__device__ __forceinline__ NormView norm_view(const PlanView &p, int layer, int D) {
+    const float *b = (const float *)p.rope - (int64_t)(layer + 1) * norm_stride(D);
+    return NormView{b, b + D, b[2 * D]};
+}
+// r of a row, sum(c) being the sum of squares of its elements times c
+template <class F>
+__device__ __forceinline__ float norm_factor(int D, float eps, F &&sum) {
+    const float s = sum(1.f);
+    float t = fmaf(s, 1.f / (float)D, eps), c = 1.f;
+    const bool big = !(s < 0x1p120f);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(big) != 0, 0)) {
+        const float s2 = sum(0x1p-70f);
+        t = big ? s2 * (1.f / (float)D) : t;
+        c = big ? 0x1p-70f : c;
+    }
+    return __builtin_amdgcn_rsqf(t) * c;
+}
+// (c x)^2 + (c y)^2, three roundings
+__device__ __forceinline__ float pair_square(float x, float y, float c) {
+#pragma clang fp contract(off)
+    x *= c, y *= c;
+    const float xx = x * x, yy = y * y;
+    return xx + yy;
+}
+// ... of eight elements, for rows whose sum no other kernel has to find
+__device__ __forceinline__ float sum_square8(const float (&x)[8], float c) {
+    return (pair_square(x[0], x[1], c) + pair_square(x[2], x[3], c)) +
+           (pair_square(x[4], x[5], c) + pair_square(x[6], x[7], c));
+}
+__device__ __forceinline__ float normed(float x, float r, float w) { return x * r * w; }
+// sum over the 16 lanes of a row, by the bits of the lane from the lowest (the
+// mirrors exchange halves whose lanes are equal by then)
+constexpr int kRowMirror = 0x140, kRowHalfMirror = 0x141;
+__device__ __forceinline__ float row16_sum(float x) {
+    x += dpp<kQuadXor1>(x);
+    x += dpp<kQuadXor2>(x);
+    x += dpp<kRowHalfMirror>(x);
+    return x + dpp<kRowMirror>(x);
+}
+// r of an input row that one wave reads: lane i brings dims i and i + D/2 (zero past
+// the pairs)
+__device__ __forceinline__ float wave_norm_factor(int D, float eps, float x, float y) {
+    return norm_factor(D, eps, [&](float c) __attribute__((always_inline)) {
+        return rows_pair<true, true>(rows_pair<true, false>(row16_sum(pair_square(x, y, c))));
+    });
 }
 
 // ---------------------------------------------------------------------------

@@ -15,6 +15,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 #include <string>
 #include <utility>
@@ -127,10 +128,14 @@ struct mtn_pool {
     int32_t max_tok = 0;           // capacity of one plan in tokens
     int32_t *d_table = nullptr;
     int32_t *d_meta = nullptr;     // packed plan metadata
+    float *d_norm = nullptr;       // norm weights (see norm_stride), the rotary table behind them
     float2 *d_rope = nullptr;      // [max_tok][D/2]
     double *d_inv_freq = nullptr;  // [2][D/2]: radians per position, then the factor on (cos, sin)
     int32_t rope_half = 0;         // rotated pairs (rotary_dim / 2)
     bool rope_il = false;          // pairs are neighbouring elements
+    bool norm = false;             // queries and keys are normed before they are rotated
+    float norm_eps = 0.f;
+    std::vector<float> norm_q, norm_k;  // weights [n_layers][D], in the order of the elements
     float *d_part = nullptr;       // decode split partials
     float *d_scratch = nullptr;    // the static partials workspace (not owned)
     size_t scratch_floats = 0;
@@ -849,7 +854,7 @@ PoolGeom geom(const mtn_pool *P) {
     g.hkv = P->cfg.n_kv_heads;
     g.d = (uint16_t)P->cfg.head_dim;
     g.rope_half = (uint8_t)P->rope_half;
-    g.rope_il = P->rope_il ? 1 : 0;
+    g.rope_il = (P->rope_il ? kRopeInterleaved : 0) | (P->norm ? kRopeNorm : 0);
     return g;
 }
 
@@ -907,6 +912,63 @@ std::vector<double> rope_table(const mtn_pool_config &c, const mtn_rope_config &
         t[(size_t)half + i] = mag;
     }
     return t;
+}
+
+// Words in front of the rotary table, which stays 256-byte aligned.
+size_t norm_words(const mtn_pool_config &c) {
+    return (size_t)ceil_div((int64_t)c.n_layers * norm_stride(c.head_dim), 64) * 64;
+}
+// ... as the kernels read them: layer l at -(l + 1) * norm_stride(D) from the end,
+// {q weights, k weights, eps}, weights in the order of the kernels' dims, which
+// hold pair i in dims i and i + D/2 (see PoolGeom).
+std::vector<float> norm_table(const mtn_pool_config &c, const std::vector<float> &q, const std::vector<float> &k,
+                              float eps, int rope_half, bool il) {
+    const int D = c.head_dim, st = norm_stride(D);
+    std::vector<float> t(norm_words(c), 0.f);
+    for (int32_t l = 0; l < c.n_layers; ++l) {
+        float *b = t.data() + t.size() - (size_t)(l + 1) * st;
+        for (int i = 0; i < D / 2; ++i) {
+            const int x = il ? 2 * i : i < rope_half ? i : i + rope_half;
+            const int y = il ? 2 * i + 1 : i < rope_half ? i + rope_half : i + D / 2;
+            b[i] = q[(size_t)l * D + x], b[i + D / 2] = q[(size_t)l * D + y];
+            b[D + i] = k[(size_t)l * D + x], b[D + i + D / 2] = k[(size_t)l * D + y];
+        }
+        b[2 * D] = eps;
+    }
+    return t;
+}
+
+// What may change how keys and queries are formed: no plan open, no session with keys.
+mtn_status check_reform(mtn_pool *P) {
+    if (P->plan_open) return fail(P, MTN_ERR_BAD_STATE, "plan open");
+    for (int32_t sid = 0; sid < P->cfg.max_sessions; ++sid)
+        if (P->is_open[sid] && P->len[sid])
+            return fail(P, MTN_ERR_BAD_STATE, "a session holds tokens of the present form");
+    return MTN_OK;
+}
+
+// Host tables into device memory on the previous plan's stream (plans of closed
+// sessions may still read them), waited for.  A capture under way on some other
+// stream is left alone.
+struct Upload {
+    void *dst;
+    const void *src;
+    size_t bytes;
+};
+mtn_status upload_tables(mtn_pool *P, std::initializer_list<Upload> ups, const char *what) {
+    if (P->host_only) return MTN_OK;
+    void *const last = P->have_last_stream ? P->last_stream : nullptr;
+    if (mtn_status cs = refuse_capture(P, last)) return cs;
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    HIP_TRY(P, hipThreadExchangeStreamCaptureMode(&mode));
+    hipError_t e = hipSuccess;
+    for (const Upload &u : ups)
+        if (e == hipSuccess && u.bytes)
+            e = hipMemcpyAsync(u.dst, u.src, u.bytes, hipMemcpyHostToDevice, (hipStream_t)last);
+    const hipError_t e2 = hipStreamSynchronize((hipStream_t)last);
+    if (e == hipSuccess) e = e2;
+    (void)hipThreadExchangeStreamCaptureMode(&mode);
+    return e == hipSuccess ? MTN_OK : hip_fail(P, e, what);
 }
 
 mtn_status check_call(mtn_pool *P, int32_t layer, void *stream) {
@@ -1356,8 +1418,10 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
             if ((e = hipEventCreateWithFlags(&v, hipEventDisableTiming)) != hipSuccess)
                 return bail(e, "event");
         size_t half = (size_t)cfg->head_dim / 2;
-        if ((e = hipMalloc(&P->d_rope, sizeof(float2) * half * (size_t)P->max_tok)) != hipSuccess)
+        if ((e = hipMalloc(&P->d_norm, sizeof(float) * norm_words(*cfg) +
+                                           sizeof(float2) * half * (size_t)P->max_tok)) != hipSuccess)
             return bail(e, "rope");
+        P->d_rope = (float2 *)(P->d_norm + norm_words(*cfg));
         const std::vector<double> inv = rope_table(*cfg, mtn_rope_config{});
         if ((e = hipMalloc(&P->d_inv_freq, sizeof(double) * inv.size())) != hipSuccess)
             return bail(e, "inv_freq");
@@ -1420,7 +1484,7 @@ void mtn_pool_destroy(mtn_pool *P) {
         (void)hipDeviceSynchronize();
         (void)hipFree(P->d_table);
         (void)hipFree(P->d_meta);
-        (void)hipFree(P->d_rope);
+        (void)hipFree(P->d_norm);
         (void)hipFree(P->d_inv_freq);
         (void)hipFree(P->d_part);
         (void)hipFree(P->d_zero);
@@ -1445,28 +1509,49 @@ void mtn_pool_destroy(mtn_pool *P) {
 mtn_status mtn_pool_set_rope(mtn_pool *P, const mtn_rope_config *rope) {
     return guarded(P, [&]() -> mtn_status {
         if (!P || !rope) return fail(P, MTN_ERR_INVALID_ARG, "null argument");
-        if (P->plan_open) return fail(P, MTN_ERR_BAD_STATE, "plan open");
-        for (int32_t sid = 0; sid < P->cfg.max_sessions; ++sid)
-            if (P->is_open[sid] && P->len[sid])
-                return fail(P, MTN_ERR_BAD_STATE, "a session holds keys rotated the present way");
+        if (mtn_status st = check_reform(P)) return st;
         const mtn_status st = check_rope(P->cfg, *rope);
         if (st) return fail(P, st, "bad rotary config");
         const std::vector<double> t = rope_table(P->cfg, *rope);
-        if (!P->host_only) {
-            // On the previous plan's stream: plans of closed sessions may still read
-            // the table.  A capture under way on some other stream is left alone.
-            void *const last = P->have_last_stream ? P->last_stream : nullptr;
-            if (mtn_status cs = refuse_capture(P, last)) return cs;
-            hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
-            HIP_TRY(P, hipThreadExchangeStreamCaptureMode(&mode));
-            hipError_t e = hipMemcpyAsync(P->d_inv_freq, t.data(), sizeof(double) * t.size(),
-                                          hipMemcpyHostToDevice, (hipStream_t)last);
-            if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)last);
-            (void)hipThreadExchangeStreamCaptureMode(&mode);
-            if (e != hipSuccess) return hip_fail(P, e, "rotary table");
+        const int32_t half = (rope->rotary_dim ? rope->rotary_dim : P->cfg.head_dim) / 2;
+        const bool il = rope->layout == MTN_ROPE_INTERLEAVED;
+        std::vector<float> w;  // the norms' weights follow the order of the dims
+        if (P->norm) w = norm_table(P->cfg, P->norm_q, P->norm_k, P->norm_eps, half, il);
+        if (mtn_status us = upload_tables(P, {{P->d_inv_freq, t.data(), sizeof(double) * t.size()},
+                                              {P->d_norm, w.data(), sizeof(float) * w.size()}}, "rotary table"))
+            return us;
+        P->rope_half = half;
+        P->rope_il = il;
+        return MTN_OK;
+    });
+}
+
+mtn_status mtn_pool_set_qk_norm(mtn_pool *P, const mtn_qk_norm_config *cfg) {
+    return guarded(P, [&]() -> mtn_status {
+        if (!P) return MTN_ERR_INVALID_ARG;
+        if (mtn_status st = check_reform(P)) return st;
+        if (!cfg) {
+            if (mtn_status st = upload_tables(P, {}, "norm weights")) return st;  // (refused alike)
+            P->norm = false;
+            return MTN_OK;
         }
-        P->rope_half = (rope->rotary_dim ? rope->rotary_dim : P->cfg.head_dim) / 2;
-        P->rope_il = rope->layout == MTN_ROPE_INTERLEAVED;
+        // (written so that NaN fails; as a float it is normal)
+        if (!(cfg->eps >= 1.1754943508222875e-38) || !(cfg->eps <= 1.0))
+            return fail(P, MTN_ERR_INVALID_ARG, "eps outside (0, 1]");
+        const size_t n = (size_t)P->cfg.n_layers * P->cfg.head_dim;
+        std::vector<float> q(n, 1.f), k(n, 1.f);
+        if (cfg->q_weight) std::copy_n(cfg->q_weight, n, q.begin());
+        if (cfg->k_weight) std::copy_n(cfg->k_weight, n, k.begin());
+        for (const auto *v : {&q, &k})
+            for (const float x : *v)
+                if (!std::isfinite(x)) return fail(P, MTN_ERR_INVALID_ARG, "a weight is not finite");
+        const std::vector<float> w = norm_table(P->cfg, q, k, (float)cfg->eps, P->rope_half, P->rope_il);
+        if (mtn_status st = upload_tables(P, {{P->d_norm, w.data(), sizeof(float) * w.size()}}, "norm weights"))
+            return st;
+        P->norm = true;
+        P->norm_eps = (float)cfg->eps;
+        P->norm_q = std::move(q);
+        P->norm_k = std::move(k);
         return MTN_OK;
     });
 }

@@ -73,7 +73,7 @@ __device__ __forceinline__ uint8_t *tail_of(const TailView &t, const PoolGeom &g
 // abandoned.)  Moves a few KiB per workgroup: bound by its chain of
 // round trips (metadata, rows, two barriers); 10.4 us for 128 x 25 tokens of 4
 // heads.
-template <int D, bool RF>
+template <int D, int RF>
 __global__ __launch_bounds__(256) void k_append_i8(PoolGeom g, PlanView p, int32_t layer,
                                                    const bf16_t *__restrict__ k,
                                                    const bf16_t *__restrict__ v, TailView tails,
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void k_append_i8(PoolGeom g, PlanView p, int32
         }
 #pragma unroll
         for (int e = 0; e < 2 * NW; ++e) vw[e] = vr[e];
-        if (RF && g.rope_il) {
+        if (RF && rope_il<RF>(g)) {
             // in memory order: words 0 .. 2 NW - 1 hold (a, b) each
             uint32_t m[2 * NW];
 #pragma unroll
@@ -121,11 +121,29 @@ __global__ __launch_bounds__(256) void k_append_i8(PoolGeom g, PlanView p, int32
                 rope_split(ka[e], kb[e], false);
             }
         }
+        float nr = 1.f;
+        NormView nw{};
+        if constexpr (RF == 2) {  // the row's sixteen lanes are all here
+            nw = norm_view(p, layer, D);
+            nr = norm_factor(D, nw.eps, [&](float f) __attribute__((always_inline)) {
+                float ss[NW];  // (the order of wave_norm_factor)
+#pragma unroll
+                for (int e = 0; e < NW; ++e)
+                    ss[e] = pair_square(__uint_as_float(ka[e] << 16), __uint_as_float(kb[e] << 16), f) +
+                            pair_square(__uint_as_float(ka[e] & 0xFFFF0000u), __uint_as_float(kb[e] & 0xFFFF0000u), f);
+                return row16_sum(NW == 2 ? ss[0] + ss[NW - 1] : ss[0]);
+            });
+        }
 #pragma unroll
         for (int e = 0; e < NW; ++e) {
             const float2 c0 = rp[2 * e], c1 = rp[2 * e + 1];
-            const float a0 = __uint_as_float(ka[e] << 16), a1 = __uint_as_float(ka[e] & 0xFFFF0000u);
-            const float b0 = __uint_as_float(kb[e] << 16), b1 = __uint_as_float(kb[e] & 0xFFFF0000u);
+            float a0 = __uint_as_float(ka[e] << 16), a1 = __uint_as_float(ka[e] & 0xFFFF0000u);
+            float b0 = __uint_as_float(kb[e] << 16), b1 = __uint_as_float(kb[e] & 0xFFFF0000u);
+            if constexpr (RF == 2) {
+                const float *wa = nw.k + P * c + 2 * e, *wb = wa + D / 2;
+                a0 = normed(a0, nr, wa[0]), a1 = normed(a1, nr, wa[1]);
+                b0 = normed(b0, nr, wb[0]), b1 = normed(b1, nr, wb[1]);
+            }
             ka[e] = pack_bf16x2(fmaf(a0, c0.x, -b0 * c0.y), fmaf(a1, c1.x, -b1 * c1.y));
             kb[e] = pack_bf16x2(fmaf(b0, c0.x, a0 * c0.y), fmaf(b1, c1.x, a1 * c1.y));
         }
@@ -247,7 +265,7 @@ constexpr int kI8Waves = 4, kI8Ring = 2;
 // no longer applied to them).
 constexpr int kTailBlocks = 5;
 
-template <int D, int G, bool RF>
+template <int D, int G, int RF>
 __global__ __launch_bounds__(64 * kI8Waves) void k_attn_i8(I8Args ia) {
     constexpr int NG = kI8Waves, NBUF = kI8Ring;
     constexpr int ND = D / 32;   // QK MFMAs per block
@@ -361,15 +379,59 @@ __global__ __launch_bounds__(64 * kI8Waves) void k_attn_i8(I8Args ia) {
     const int d0 = D / 4 * g4;
     const float2 *rp = a.p.rope + (int64_t)t * (D / 2) + (d0 & (D / 2 - 1));
     const float sgn = g4 < 2 ? -1.f : 1.f;
-    // 8 rotated elements of slice s of an input row
-    auto rotate8 = [&](const bf16_t *r, int s, float (&y)[8]) __attribute__((always_inline)) {
+    // elements of slice s of an input row and their partners
+    auto load_pair = [&](const bf16_t *r, int s, float (&x)[8], float (&z)[8]) __attribute__((always_inline)) {
         const RopeSrc o = rope_src<RF>(g, d0 + 8 * s, 8, D);
         uint4 xv = *(const uint4 *)(r + o.x), pv = *(const uint4 *)(r + o.y);
         if constexpr (RF)
-            if (g.rope_il) rope_split(xv, pv, g4 >= 2);
-        float x[8], z[8];
+            if (rope_il<RF>(g)) rope_split(xv, pv, g4 >= 2);
         unpack8(xv, x);
         unpack8(pv, z);
+    };
+    NormView norms{};
+    if constexpr (RF == 2) norms = norm_view(a.p, a.layer, D);
+    auto row_factor = [&](const bf16_t *r) __attribute__((always_inline)) {
+        return norm_factor(D, norms.eps, [&](float c) __attribute__((always_inline)) {
+            float ss = 0.f;
+#pragma unroll
+            for (int s = 0; s < ND; ++s) {
+                float x[8], z[8];
+                load_pair(r, s, x, z);
+                ss += sum_square8(x, c);
+            }
+            return rows_sum(ss);
+        });
+    };
+    // ... of the newest key, in the order of wave_norm_factor
+    auto key_factor = [&](const bf16_t *r) __attribute__((always_inline)) {
+        return norm_factor(D, norms.eps, [&](float c) __attribute__((always_inline)) {
+            float s8[ND];
+#pragma unroll
+            for (int s = 0; s < ND; ++s) {
+                float x[8], z[8], y[4];
+                load_pair(r, s, x, z);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)  // dims 2 e and 2 e + 1, each with its partner
+                    y[e] = pair_square(x[2 * e], z[2 * e], c) + pair_square(x[2 * e + 1], z[2 * e + 1], c);
+                s8[s] = (y[0] + y[1]) + (y[2] + y[3]);
+            }
+            float ss = s8[0];
+            if constexpr (ND == 2) ss = s8[0] + s8[1];
+            if constexpr (ND == 4) ss = (s8[0] + s8[1]) + (s8[2] + s8[3]);
+            return rows_pair<true, false>(ss);  // (rows two apart hold the partners)
+        });
+    };
+    // 8 rotated elements of slice s of an input row (w, f: its norm)
+    auto rotate8 = [&](const bf16_t *r, int s, const float *w, float f, float (&y)[8]) __attribute__((always_inline)) {
+        float x[8], z[8];
+        load_pair(r, s, x, z);
+        if constexpr (RF == 2) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = normed(x[e], f, w[d0 + 8 * s + e]);
+                z[e] = normed(z[e], f, w[(d0 ^ (D / 2)) + 8 * s + e]);
+            }
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float2 cs = rp[8 * s + e];
@@ -381,10 +443,11 @@ __global__ __launch_bounds__(64 * kI8Waves) void k_attn_i8(I8Args ia) {
     {
         const bool hv = n < G;
         const bf16_t *qr = (const bf16_t *)a.q + (row * g.hq + (int64_t)kvh * G + (hv ? n : 0)) * D;
-        float q[ND][8], mx = 0.f;
+        float q[ND][8], mx = 0.f, f = 1.f;
+        if constexpr (RF == 2) f = row_factor(qr);
 #pragma unroll
         for (int s = 0; s < ND; ++s) {
-            rotate8(qr, s, q[s]);
+            rotate8(qr, s, norms.q, f, q[s]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 q[s][e] = hv ? q[s][e] * a.scale_log2 : 0.f;
@@ -437,10 +500,12 @@ __global__ __launch_bounds__(64 * kI8Waves) void k_attn_i8(I8Args ia) {
             const bf16_t *vh = (const bf16_t *)a.v_new + (row * g.hkv + kvh) * D + NJ * n;
 #pragma unroll
             for (int x = 0; x < NJ / 2; x += 2) *(uint2 *)&vn[x] = *(const uint2 *)(vh + 2 * x);
+            float f = 1.f;
+            if constexpr (RF == 2) f = key_factor(kh);
 #pragma unroll
             for (int s = 0; s < ND; ++s) {
                 float y[8];
-                rotate8(kh, s, y);
+                rotate8(kh, s, norms.k, f, y);
                 const uint4 kn = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]),
                                             pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
                 if (n == toff) {
@@ -716,10 +781,9 @@ hipError_t launch_i8_g(const I8Args &ia, hipStream_t s) {
     if (units == 0) return hipSuccess;
     if (units > INT32_MAX) return hipErrorInvalidValue;  // one grid dimension, 32-bit unit index
     const dim3 grid((unsigned)units), block(64 * kI8Waves);
-    if (rope_form(ia.a.g))
-        hipLaunchKernelGGL((k_attn_i8<D, G, true>), grid, block, 0, s, ia);
-    else
-        hipLaunchKernelGGL((k_attn_i8<D, G, false>), grid, block, 0, s, ia);
+    with_form(ia.a.g, [&](auto rf) {
+        hipLaunchKernelGGL((k_attn_i8<D, G, decltype(rf)::value>), grid, block, 0, s, ia);
+    });
     return hipGetLastError();
 }
 template <class F>
@@ -756,7 +820,7 @@ hipError_t launch_append_i8(const PoolGeom &g, const PlanView &p, int32_t layer,
     auto by_d = [&](auto rf) {
         g.d == 128 ? launch(std::integral_constant<int, 128>{}, rf) : launch(std::integral_constant<int, 64>{}, rf);
     };
-    rope_form(g) ? by_d(std::true_type{}) : by_d(std::false_type{});
+    with_form(g, by_d);
     return hipGetLastError();
 }
 

@@ -29,8 +29,13 @@ struct PoolGeom {
     // the table leaves alone, in order.  The kernels hold pair i in dims i and
     // i + D/2, queries and stored keys alike: scores do not depend on the order.
     uint8_t rope_half;       // rotary_dim / 2
-    uint8_t rope_il;
+    uint8_t rope_il;         // kRopeInterleaved | kRopeNorm
 };
+constexpr uint8_t kRopeInterleaved = 1, kRopeNorm = 2;
+
+// Norm weights lie in front of the rotary table (PlanView::rope), layer l at
+// float offset -(l + 1) * norm_stride(D): the query's D, the key's D, eps.
+constexpr int norm_stride(int d) { return 2 * d + 4; }
 
 // One planned token: which session, absolute position, io row, slot.
 struct PlanView {

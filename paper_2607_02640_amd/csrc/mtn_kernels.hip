@@ -64,7 +64,7 @@ __global__ void k_plan_apply(const uint4 *__restrict__ src, uint4 *__restrict__ 
 // [off0, off0 + len) in memory order: whole row segments instead of one
 // 2-byte element per 32 bytes.
 constexpr int kAppendWaves = 4;
-template <typename T, bool RF>
+template <typename T, int RF>
 __global__ __launch_bounds__(64 * kAppendWaves) void k_append(PoolGeom g, PlanView p, int32_t layer,
                                                             const T *__restrict__ k,
                                                             const T *__restrict__ v,
@@ -81,6 +81,22 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_append(PoolGeom g, PlanVi
     T *K = (T *)tile;
     T *VT = (T *)(tile + g.tile_bytes);
     const int off0 = p.tok_off[t0];
+    // norms: the wave's rows loaded side by side (one pair a lane: D <= 128)
+    NormView nw{};
+    float wk0 = 1.f, wk1 = 1.f;  // the key's weights of the lane's pair
+    float nx[kBlock / kAppendWaves] = {}, ny[kBlock / kAppendWaves] = {};
+    if constexpr (RF == 2) {
+        nw = norm_view(p, layer, D);
+        if (lane < half) {
+            wk0 = nw.k[lane], wk1 = nw.k[lane + half];
+#pragma unroll
+            for (int jj = 0; jj < kBlock / kAppendWaves; ++jj) {
+                const int64_t row = p.tok_row[t0 + min(w + kAppendWaves * jj, len - 1)];
+                const T *kr = k + (row * g.hkv + h) * D;
+                nx[jj] = to_f32(kr[rope_a<RF>(g, lane)]), ny[jj] = to_f32(kr[rope_b<RF>(g, lane, D)]);
+            }
+        }
+    }
 #pragma unroll
     for (int jj = 0; jj < kBlock / kAppendWaves; ++jj) {
         const int j = w + kAppendWaves * jj;
@@ -90,9 +106,15 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_append(PoolGeom g, PlanVi
         const T *kr = k + (row * g.hkv + h) * D;
         const T *vr = v + (row * g.hkv + h) * D;
         T *kd = K + (off0 + j) * D;
+        float r = 1.f;
+        if constexpr (RF == 2) r = wave_norm_factor(D, nw.eps, nx[jj], ny[jj]);
         for (int i = lane; i < half; i += 64) {
             const float2 cs = p.rope[(int64_t)t * half + i];
-            const float x0 = to_f32(kr[rope_a<RF>(g, i)]), x1 = to_f32(kr[rope_b<RF>(g, i, D)]);
+            float x0, x1;
+            if constexpr (RF == 2)
+                x0 = normed(nx[jj], r, wk0), x1 = normed(ny[jj], r, wk1);
+            else
+                x0 = to_f32(kr[rope_a<RF>(g, i)]), x1 = to_f32(kr[rope_b<RF>(g, i, D)]);
             kd[i] = from_f32<T>(fmaf(x0, cs.x, -x1 * cs.y));
             kd[i + half] = from_f32<T>(fmaf(x1, cs.x, x0 * cs.y));
             tr[i * kBlock + j] = vr[i];
@@ -168,7 +190,7 @@ struct DecodeShape {
 // them.  At the end the groups' (max, sum, acc) are merged through LDS by
 // log-sum-exp, so several waves per SIMD stream one unit with no second
 // launch.
-template <typename T, int D, int G, int WPU, int NG, int NBUF, bool RF>
+template <typename T, int D, int G, int WPU, int NG, int NBUF, int RF>
 __global__ __launch_bounds__(64 * WPU * NG) void k_attn_valu(AttnArgs a) {
     using L = Lay<T, D>;
     constexpr int HW = G / WPU;                     // heads per wave
@@ -289,33 +311,55 @@ __global__ __launch_bounds__(64 * WPU * NG) void k_attn_valu(AttnArgs a) {
                     x[e] = __uint_as_float(w[e]);
             }
         };
+        // the elements of vector vq of row r and their partners, as floats
+        auto load_pair = [&](const T *r, int vq, float *xs, float *ys) __attribute__((always_inline)) {
+            if constexpr (RF) {
+                const RopeSrc o = rope_src<RF>(g, d0 + vq * EPV, EPV, D);
+                uint4 x = *(const uint4 *)(r + o.x), y = *(const uint4 *)(r + o.y);
+                if (rope_il<RF>(g)) {
+                    if constexpr (sizeof(T) == 2)
+                        rope_split(x, y, qtr >= 2);
+                    else
+                        rope_split_f32(x, y, qtr >= 2);
+                }
+                unpack(x, xs);
+                unpack(y, ys);
+            } else {
+                unpack(((const uint4 *)(r + d0))[vq], xs);
+                unpack(((const uint4 *)(r + dp))[vq], ys);
+            }
+        };
+        // norms: every lane of the wave takes one pair of a row, as the append does
+        NormView nw{};
+        if constexpr (RF == 2) nw = norm_view(a.p, a.layer, D);
+        auto row_factor = [&](const T *r) __attribute__((always_inline)) {
+            float x = 0.f, y = 0.f;
+            if (lane < D / 2) x = to_f32(r[rope_a<RF>(g, lane)]), y = to_f32(r[rope_b<RF>(g, lane, D)]);
+            return wave_norm_factor(D, nw.eps, x, y);
+        };
+        auto norm_pair = [&](const float *w, float f, int vq, float *xs, float *ys) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < EPV; ++e) {
+                xs[e] = normed(xs[e], f, w[d0 + vq * EPV + e]);
+                ys[e] = normed(ys[e], f, w[dp + vq * EPV + e]);
+            }
+        };
+        float qr[HW], krf = 1.f;
+        if constexpr (RF == 2) {
+#pragma unroll
+            for (int h = 0; h < HW; ++h) qr[h] = row_factor(qb + (int64_t)h * D);
+            if (own_new) krf = row_factor(kb);
+        }
 #pragma unroll
         for (int vq = 0; vq < NVQ; ++vq) {
-            // the vector's elements of row r and their partners, as floats
-            auto load_pair = [&](const T *r, float *xs, float *ys) __attribute__((always_inline)) {
-                if constexpr (RF) {
-                    const RopeSrc o = rope_src<RF>(g, d0 + vq * EPV, EPV, D);
-                    uint4 x = *(const uint4 *)(r + o.x), y = *(const uint4 *)(r + o.y);
-                    if (g.rope_il) {
-                        if constexpr (sizeof(T) == 2)
-                            rope_split(x, y, qtr >= 2);
-                        else
-                            rope_split_f32(x, y, qtr >= 2);
-                    }
-                    unpack(x, xs);
-                    unpack(y, ys);
-                } else {
-                    unpack(((const uint4 *)(r + d0))[vq], xs);
-                    unpack(((const uint4 *)(r + dp))[vq], ys);
-                }
-            };
             float2 cs[EPV];
 #pragma unroll
             for (int e = 0; e < EPV; ++e) cs[e] = rp[vq * EPV + e];
             uint32_t kv4[4];  // the newest key's rotated vector (stored layout)
             if (own_new) {
                 float xs[EPV], ys[EPV];
-                load_pair(kb, xs, ys);
+                load_pair(kb, vq, xs, ys);
+                if constexpr (RF == 2) norm_pair(nw.k, krf, vq, xs, ys);
 #pragma unroll
                 for (int e = 0; e < EPV; e += 2) {
                     const float k0 = fmaf(xs[e], cs[e].x, sgn * ys[e] * cs[e].y);
@@ -333,7 +377,8 @@ __global__ __launch_bounds__(64 * WPU * NG) void k_attn_valu(AttnArgs a) {
 #pragma unroll
             for (int h = 0; h < HW; ++h) {
                 float xs[EPV], ys[EPV];
-                load_pair(qb + (int64_t)h * D, xs, ys);
+                load_pair(qb + (int64_t)h * D, vq, xs, ys);
+                if constexpr (RF == 2) norm_pair(nw.q, qr[h], vq, xs, ys);
 #pragma unroll
                 for (int e = 0; e < EPV; e += 2) {
                     const int i = vq * EPV + e;
@@ -974,7 +1019,7 @@ enum KvForm { kKvBf16, kKvF8, kKvI8 };
 // regions (per block four 1 KiB DMA instructions plus the 32 exponent
 // bytes), and every stage is converted into one of two bf16 stage buffers (a
 // second barrier) before the same MFMA stage body runs on it.
-template <int D, int G, int FORM, bool RF>
+template <int D, int G, int FORM, int RF>
 __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
     using Lds = PfLds<D>;
     constexpr bool F8 = FORM == kKvF8, I8 = FORM == kKvI8, Q8 = F8 || I8;
@@ -1228,6 +1273,12 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             b.off[u] = scalar_ld(a.p.tok_off, t);
         }
     };
+    NormView nw{};
+    float nw_k0 = 1.f, nw_k1 = 1.f;  // the key's weights of the appending lane's pair
+    if constexpr (RF == 2) {
+        nw = norm_view(a.p, a.layer, D);
+        if (fuse) nw_k0 = nw.k[lane], nw_k1 = nw.k[lane + D / 2];
+    }
     auto app_store = [&](int j0, AppBatch &b) __attribute__((always_inline)) {
         uint8_t *lw = const_cast<uint8_t *>(layer_base);
         auto f = [](uint32_t bits) { return __uint_as_float(bits << 16); };
@@ -1239,7 +1290,11 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
 #pragma unroll
         for (int u = 0; u < AB; ++u) {
             if (j0 + u * NAW >= ntok) break;
-            const float k0 = f(b.k0[u]), k1 = f(b.k1[u]);
+            float k0 = f(b.k0[u]), k1 = f(b.k1[u]);
+            if constexpr (RF == 2) {
+                const float r = wave_norm_factor(D, nw.eps, k0, k1);
+                k0 = normed(k0, r, nw_k0), k1 = normed(k1, r, nw_k1);
+            }
             const float y0 = fmaf(k0, b.cs[u].x, -k1 * b.cs[u].y);
             const float y1 = fmaf(k1, b.cs[u].x, k0 * b.cs[u].y);
             store_token_fp8(lw + (int64_t)b.blk[u] * g.block_stride, b.off[u], y0, y1,
@@ -1340,6 +1395,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
         }
         uint4 qx[kPfTpw][ND], qy[kPfTpw][ND];  // dims d0 .. d0 + 7 and their partners d0 ^ (D / 2)
         float4 qc[kPfTpw][ND / 2][4];          // (cos, sin) of dims (d0 % (D / 2)) .. + 7
+        float4 qw[RF == 2 ? ND : 1][2];        // norm weights of dims d0 .. + 7
         uint4 tail_part = make_uint4(0, 0, 0, 0);  // this thread's 16 bytes of the open block
         if constexpr (I8)
             if (tail_v >= 0 && tid < 4 * D) tail_part = ((const uint4 *)tail_rows)[tid];
@@ -1362,6 +1418,11 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) qc[i][h2][k] = ((const float4 *)(rp + h2 * 32 + 8 * lg))[k];
         }
+        if constexpr (RF == 2)
+#pragma unroll
+            for (int s = 0; s < ND; ++s)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) qw[s][k] = ((const float4 *)(nw.q + s * 32 + 8 * lg))[k];
         // The DMA waves copy the first kPfEarly stages right behind the q
         // loads: the first barriers need them, and the rotation's waits for
         // the q loads (counted by the compiler, which does not see the copies)
@@ -1372,7 +1433,7 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
             for (int st = 0; st < kPfEarly; ++st) issue_block(st, phys(2 * st + db));
         }
         __builtin_amdgcn_sched_barrier(0);
-        if (RF && g.rope_il) {
+        if (RF && rope_il<RF>(g)) {
 #pragma unroll
             for (int i = 0; i < kPfTpw; ++i)
 #pragma unroll
@@ -1387,13 +1448,32 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
 #pragma unroll
         for (int i = 0; i < kPfTpw; ++i) {
             q_sc[i] = 1.f;
-            float q_mul = a.scale_log2;
+            float q_mul = a.scale_log2, qr = 1.f;
+            if constexpr (RF == 2) {
+                qr = norm_factor(D, nw.eps, [&](float c) __attribute__((always_inline)) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int s = 0; s < ND; ++s) {
+                        float x[8];
+                        unpack8(qx[i][s], x);
+                        ss += sum_square8(x, c);
+                    }
+                    return rows_sum(ss);
+                });
+            }
+            auto norm8 = [&](int s, float (&x)[8]) __attribute__((always_inline)) {
+                const float4 w0 = qw[s][0], w1 = qw[s][1];
+                const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = normed(x[e], qr, w[e]);
+            };
             if constexpr (I8) {
                 float mx = 0.f;
 #pragma unroll
                 for (int s = 0; s < ND; ++s) {
                     float x[8];
                     unpack8(qx[i][s], x);
+                    if constexpr (RF == 2) norm8(s, x);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(x[e]));
                 }
@@ -1409,6 +1489,10 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                 float xv[8], yv[8], cs[16];
                 unpack8(qx[i][s], xv);
                 unpack8(qy[i][s], yv);
+                if constexpr (RF == 2) {
+                    norm8(s, xv);
+                    norm8(s ^ (ND / 2), yv);
+                }
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const float4 c = qc[i][s % (ND / 2)][k];
@@ -2064,10 +2148,10 @@ hipError_t launch_valu_t(const AttnArgs &a, hipStream_t s) {
     if (units == 0) return hipSuccess;
     if (units > INT32_MAX) return hipErrorInvalidValue;  // one grid dimension, 32-bit unit index
     const dim3 grid((unsigned)units), block(64 * DS::WPU * DS::NG);
-    if (rope_form(a.g))
-        hipLaunchKernelGGL((k_attn_valu<T, D, G, DS::WPU, DS::NG, DS::NBUF, true>), grid, block, 0, s, a);
-    else
-        hipLaunchKernelGGL((k_attn_valu<T, D, G, DS::WPU, DS::NG, DS::NBUF, false>), grid, block, 0, s, a);
+    with_form(a.g, [&](auto rf) {
+        hipLaunchKernelGGL((k_attn_valu<T, D, G, DS::WPU, DS::NG, DS::NBUF, decltype(rf)::value>), grid, block, 0,
+                           s, a);
+    });
     return hipGetLastError();
 }
 
@@ -2087,7 +2171,7 @@ int resident_t() {
     using DS = DecodeShape<G>;
     int n = 0;
     if (hipOccupancyMaxActiveBlocksPerMultiprocessor(
-            &n, k_attn_valu<T, D, G, DS::WPU, DS::NG, DS::NBUF, false>, 64 * DS::WPU * DS::NG, 0) !=
+            &n, k_attn_valu<T, D, G, DS::WPU, DS::NG, DS::NBUF, 0>, 64 * DS::WPU * DS::NG, 0) !=
         hipSuccess)
         return 1;
     return n > 0 ? n : 1;
@@ -2153,10 +2237,7 @@ hipError_t launch_append(int dtype, const PoolGeom &g, const PlanView &p, int32_
         hipLaunchKernelGGL((k_append<T, decltype(rf)::value>), dim3(grid), dim3(64 * kAppendWaves), 0, s,
                            g, p, layer, (const T *)k, (const T *)v, run_tok0, run_len);
     };
-    if (dtype == 1)
-        rope_form(g) ? launch(bf16_t{}, std::true_type{}) : launch(bf16_t{}, std::false_type{});
-    else
-        rope_form(g) ? launch(float{}, std::true_type{}) : launch(float{}, std::false_type{});
+    with_form(g, [&](auto rf) { dtype == 1 ? launch(bf16_t{}, rf) : launch(float{}, rf); });
     return hipGetLastError();
 }
 
@@ -2226,7 +2307,7 @@ int prefill_rows_per_pass() { return kPfRowsPerPass; }
 // tile per wave) or the full kPfRowsPerPass
 bool prefill_pass_rows_valid(int rows) { return rows == kPfRowsPerPass || rows == kPfWaves * 16; }
 
-template <int D, int FORM, bool RF>
+template <int D, int FORM, int RF>
 void launch_prefill_g(int G, dim3 grid, dim3 block, hipStream_t s, const PfArgs &pa) {
     switch (G) {
         case 1: hipLaunchKernelGGL((k_prefill_mfma<D, 1, FORM, RF>), grid, block, 0, s, pa); break;
@@ -2252,7 +2333,7 @@ hipError_t launch_prefill_mfma(int dtype, const AttnArgs &a, const int32_t *item
     PfArgs pa{a, items, zero_page, pass_rows, tails};
     dim3 grid((unsigned)wgs), block(64 * kPfWaves);
     auto launch = [&](auto rf) {
-        constexpr bool RF = decltype(rf)::value;
+        constexpr int RF = decltype(rf)::value;
         if (dtype == 2)
             launch_prefill_g<128, kKvF8, RF>(G, grid, block, s, pa);
         else if (dtype == 3)
@@ -2263,10 +2344,7 @@ hipError_t launch_prefill_mfma(int dtype, const AttnArgs &a, const int32_t *item
         else
             launch_prefill_g<64, kKvBf16, RF>(G, grid, block, s, pa);
     };
-    if (rope_form(a.g))
-        launch(std::true_type{});
-    else
-        launch(std::false_type{});
+    with_form(a.g, launch);
     return hipGetLastError();
 }
 

@@ -51,7 +51,7 @@ __device__ __forceinline__ f32x4_t mfma_pv(const uint2 &a, const uint2 &b, f32x4
 // fused RoPE + quantize + append: one wave per (token, kv head); lane i holds
 // the rotation pair (i, i + 64)
 // ---------------------------------------------------------------------------
-template <bool RF>
+template <int RF>
 __global__ __launch_bounds__(256) void k_append_fp8(PoolGeom g, PlanView p, int32_t layer,
                                                     const bf16_t *__restrict__ k,
                                                     const bf16_t *__restrict__ v) {
@@ -64,7 +64,12 @@ __global__ __launch_bounds__(256) void k_append_fp8(PoolGeom g, PlanView p, int3
     const bf16_t *kr = k + (row * g.hkv + h) * kF8D;
     const bf16_t *vr = v + (row * g.hkv + h) * kF8D;
     const float2 cs = p.rope[(int64_t)t * (kF8D / 2) + lane];
-    const float x0 = to_f32(kr[rope_a<RF>(g, lane)]), x1 = to_f32(kr[rope_b<RF>(g, lane, kF8D)]);
+    float x0 = to_f32(kr[rope_a<RF>(g, lane)]), x1 = to_f32(kr[rope_b<RF>(g, lane, kF8D)]);
+    if constexpr (RF == 2) {
+        const NormView nw = norm_view(p, layer, kF8D);
+        const float r = wave_norm_factor(kF8D, nw.eps, x0, x1);
+        x0 = normed(x0, r, nw.k[lane]), x1 = normed(x1, r, nw.k[lane + kF8D / 2]);
+    }
     const float y0 = fmaf(x0, cs.x, -x1 * cs.y);
     const float y1 = fmaf(x1, cs.x, x0 * cs.y);
     const float v0 = to_f32(vr[lane]), v1 = to_f32(vr[lane + 64]);
@@ -111,7 +116,7 @@ struct MfmaShape {
 #endif
 };
 
-template <int D, bool F8, int G, int NG, int NBUF, bool RF>
+template <int D, bool F8, int G, int NG, int NBUF, int RF>
 __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
     static_assert(D == kF8D || (D == 64 && !F8), "head dims with a block layout");
     constexpr int ND = D / 32;   // QK MFMAs per block
@@ -189,24 +194,49 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
     // the B operand of QK MFMA s holds dims D/4 g4 + 8 s .. + 7 of head n.
     const int d0 = D / 4 * g4;
     uint4 qb[ND];
+    NormView nw{};
+    if constexpr (RF == 2) nw = norm_view(a.p, a.layer, D);
     const float2 *rp = a.p.rope + (int64_t)t * (D / 2) + (d0 & (D / 2 - 1));
     const float sgn = g4 < 2 ? -1.f : 1.f;
     {
         const bool hv = n < G;
         const bf16_t *qh = (const bf16_t *)a.q + (row * g.hq + (int64_t)kvh * G + (hv ? n : 0)) * D;
         const bf16_t *qd = qh + d0, *qp = qh + (d0 ^ (D / 2));  // the dims and their partners
-#pragma unroll
-        for (int s = 0; s < ND; ++s) {
-            float x[8], y[8];
+        auto load_pair = [&](int s, float (&x)[8], float (&y)[8]) __attribute__((always_inline)) {
             if constexpr (RF) {
                 const RopeSrc o = rope_src<RF>(g, d0 + 8 * s, 8, D);
                 uint4 xv = *(const uint4 *)(qh + o.x), yv = *(const uint4 *)(qh + o.y);
-                if (g.rope_il) rope_split(xv, yv, g4 >= 2);
+                if (rope_il<RF>(g)) rope_split(xv, yv, g4 >= 2);
                 unpack8(xv, x);
                 unpack8(yv, y);
             } else {
                 unpack8(((const uint4 *)qd)[s], x);
                 unpack8(((const uint4 *)qp)[s], y);
+            }
+        };
+        float qr = 1.f;
+        if constexpr (RF == 2) {  // a row lies over the four lanes with its n
+            qr = norm_factor(D, nw.eps, [&](float c) __attribute__((always_inline)) {
+                float ss = 0.f;
+#pragma unroll
+                for (int s = 0; s < ND; ++s) {
+                    float x[8], y[8];
+                    load_pair(s, x, y);
+                    ss += sum_square8(x, c);
+                }
+                return rows_sum(ss);
+            });
+        }
+#pragma unroll
+        for (int s = 0; s < ND; ++s) {
+            float x[8], y[8];
+            load_pair(s, x, y);
+            if constexpr (RF == 2) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = normed(x[e], qr, nw.q[d0 + 8 * s + e]);
+                    y[e] = normed(y[e], qr, nw.q[(d0 ^ (D / 2)) + 8 * s + e]);
+                }
             }
             uint32_t w[4];
 #pragma unroll
@@ -235,18 +265,38 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
                 kd = g4 < 2 ? ka : kb;
                 kp = g4 < 2 ? kb : ka;
             }
-            const float k0 = fmaf(to_f32(kh[kd]), cs.x, sgn * to_f32(kh[kp]) * cs.y);
+            float kx = to_f32(kh[kd]), ky = to_f32(kh[kp]);
+            if constexpr (RF == 2) {
+                // (the order of wave_norm_factor: dims D/2 apart lie two rows apart)
+                const float r = norm_factor(D, nw.eps, [&](float c) __attribute__((always_inline)) {
+                    const float x = kx * c;
+                    return rows_pair<true, false>(row16_sum(rows_pair<true, true>(x * x)));
+                });
+                kx = normed(kx, r, nw.k[dd]), ky = normed(ky, r, nw.k[dd ^ (D / 2)]);
+            }
+            const float k0 = fmaf(kx, cs.x, sgn * ky * cs.y);
             kc2 = from_f32<bf16_t>(k0).bits;  // rounded to the stored type as the append does
             vc2 = vh[dd].bits;
         } else {
             const RopeSrc o = rope_src<RF>(g, dd, 2, D);
             uint32_t kx = *(const uint32_t *)(kh + o.x), ky = *(const uint32_t *)(kh + o.y);
-            if (RF && g.rope_il) rope_split(kx, ky, g4 >= 2);
+            if (RF && rope_il<RF>(g)) rope_split(kx, ky, g4 >= 2);
             const uint32_t vx = *(const uint32_t *)(vh + dd);
             const float4 cs = *(const float4 *)(rp + 2 * n);  // (cos, sin) of dims dd, dd + 1
-            const float k0 = fmaf(__uint_as_float(kx << 16), cs.x, sgn * __uint_as_float(ky << 16) * cs.y);
-            const float k1 = fmaf(__uint_as_float(kx & 0xFFFF0000u), cs.z,
-                                  sgn * __uint_as_float(ky & 0xFFFF0000u) * cs.w);
+            float x0 = __uint_as_float(kx << 16), x1 = __uint_as_float(kx & 0xFFFF0000u);
+            float y0 = __uint_as_float(ky << 16), y1 = __uint_as_float(ky & 0xFFFF0000u);
+            if constexpr (RF == 2) {
+                const float r = norm_factor(D, nw.eps, [&](float c) __attribute__((always_inline)) {
+                    const float u = x0 * c, w = x1 * c;
+                    return rows_pair<true, false>(
+                        row16_sum(rows_pair<true, true>(u * u) + rows_pair<true, true>(w * w)));
+                });
+                const int dp = dd ^ (D / 2);
+                x0 = normed(x0, r, nw.k[dd]), x1 = normed(x1, r, nw.k[dd + 1]);
+                y0 = normed(y0, r, nw.k[dp]), y1 = normed(y1, r, nw.k[dp + 1]);
+            }
+            const float k0 = fmaf(x0, cs.x, sgn * y0 * cs.y);
+            const float k1 = fmaf(x1, cs.z, sgn * y1 * cs.w);
             if constexpr (F8) {
                 const float v0 = __uint_as_float(vx << 16), v1 = __uint_as_float(vx & 0xFFFF0000u);
                 float ak = fmaxf(fabsf(k0), fabsf(k1)), av = fmaxf(fabsf(v0), fabsf(v1));
@@ -575,17 +625,16 @@ hipError_t launch_mfma_g(const AttnArgs &a, hipStream_t s) {
     if (units == 0) return hipSuccess;
     if (units > INT32_MAX) return hipErrorInvalidValue;  // one grid dimension, 32-bit unit index
     const dim3 grid((unsigned)units), block(64 * S::NG);
-    if (rope_form(a.g))
-        hipLaunchKernelGGL((k_attn_mfma<D, F8, G, S::NG, S::NBUF, true>), grid, block, 0, s, a);
-    else
-        hipLaunchKernelGGL((k_attn_mfma<D, F8, G, S::NG, S::NBUF, false>), grid, block, 0, s, a);
+    with_form(a.g, [&](auto rf) {
+        hipLaunchKernelGGL((k_attn_mfma<D, F8, G, S::NG, S::NBUF, decltype(rf)::value>), grid, block, 0, s, a);
+    });
     return hipGetLastError();
 }
 template <int D, bool F8, int G>
 int resident_mfma_g() {
     using S = MfmaShape<F8, G>;
     int n = 0;
-    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_attn_mfma<D, F8, G, S::NG, S::NBUF, false>,
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_attn_mfma<D, F8, G, S::NG, S::NBUF, 0>,
                                                      64 * S::NG, 0) != hipSuccess)
         return 1;
     // The split rule fills these slots.  It counts the workgroups whose rings
@@ -656,12 +705,10 @@ hipError_t launch_append_fp8(const PoolGeom &g, const PlanView &p, int32_t layer
     const int64_t waves = (int64_t)p.n_tok * g.hkv;
     if (waves == 0) return hipSuccess;
     const dim3 grid((unsigned)((waves + 3) / 4)), block(256);
-    if (rope_form(g))
-        hipLaunchKernelGGL(k_append_fp8<true>, grid, block, 0, s, g, p, layer, (const bf16_t *)k,
+    with_form(g, [&](auto rf) {
+        hipLaunchKernelGGL(k_append_fp8<decltype(rf)::value>, grid, block, 0, s, g, p, layer, (const bf16_t *)k,
                            (const bf16_t *)v);
-    else
-        hipLaunchKernelGGL(k_append_fp8<false>, grid, block, 0, s, g, p, layer, (const bf16_t *)k,
-                           (const bf16_t *)v);
+    });
     return hipGetLastError();
 }
 

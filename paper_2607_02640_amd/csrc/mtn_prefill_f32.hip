@@ -45,7 +45,7 @@ __device__ __forceinline__ f32x4_t mfma_f32(float a, float b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-template <int D, int G, bool RF>
+template <int D, int G, int RF>
 __global__ __launch_bounds__(64 * kF32Waves) void k_prefill_f32(F32Args pa) {
     constexpr int ROW = D * 4;            // bytes of a key row
     constexpr int TILE = kBlock * ROW;    // ... of a K (or V^T) tile
@@ -143,13 +143,38 @@ __global__ __launch_bounds__(64 * kF32Waves) void k_prefill_f32(F32Args pa) {
     {
         const float *qh = (const float *)a.q + ((int64_t)(row_t0 + tj) * g.hq + hq0 + gh) * D;
         const float2 *rp = a.p.rope + (int64_t)(tok0 + tj) * (D / 2);
+        auto load_pair = [&](int d0, float4 &x, float4 &y) __attribute__((always_inline)) {
+            const RopeSrc o = rope_src<RF>(g, d0, 4, D);
+            uint4 xb = *(const uint4 *)(qh + o.x), yb = *(const uint4 *)(qh + o.y);
+            if (RF && rope_il<RF>(g)) rope_split_f32(xb, yb, d0 >= D / 2);
+            x = __builtin_bit_cast(float4, xb);
+            y = __builtin_bit_cast(float4, yb);
+        };
+        NormView nw{};
+        float qr = 1.f;
+        if constexpr (RF == 2) {
+            nw = norm_view(a.p, a.layer, D);
+            qr = norm_factor(D, nw.eps, [&](float f) __attribute__((always_inline)) {
+                float ss = 0.f;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    float4 x, y;
+                    load_pair(16 * c + 4 * lg, x, y);
+                    ss += pair_square(x.x, x.y, f) + pair_square(x.z, x.w, f);
+                }
+                return rows_sum(ss);
+            });
+        }
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int d0 = 16 * c + 4 * lg;
-            const RopeSrc o = rope_src<RF>(g, d0, 4, D);
-            uint4 xb = *(const uint4 *)(qh + o.x), yb = *(const uint4 *)(qh + o.y);
-            if (RF && g.rope_il) rope_split_f32(xb, yb, d0 >= D / 2);
-            const float4 x = __builtin_bit_cast(float4, xb), y = __builtin_bit_cast(float4, yb);
+            float4 x, y;
+            load_pair(d0, x, y);
+            if constexpr (RF == 2) {
+                const float4 wx = *(const float4 *)(nw.q + d0), wy = *(const float4 *)(nw.q + (d0 ^ (D / 2)));
+                x = make_float4(normed(x.x, qr, wx.x), normed(x.y, qr, wx.y), normed(x.z, qr, wx.z), normed(x.w, qr, wx.w));
+                y = make_float4(normed(y.x, qr, wy.x), normed(y.y, qr, wy.y), normed(y.z, qr, wy.z), normed(y.w, qr, wy.w));
+            }
             const float4 c0 = *(const float4 *)(rp + (d0 & (D / 2 - 1)));
             const float4 c1 = *(const float4 *)(rp + (d0 & (D / 2 - 1)) + 2);
             const float sg = d0 < D / 2 ? -1.f : 1.f;
@@ -367,7 +392,7 @@ __global__ __launch_bounds__(64 * kF32Waves) void k_prefill_f32(F32Args pa) {
     if (a.lse && lg == 0) a.lse[oh] = row_lse(m_ref, l);
 }
 
-template <int D, bool RF>
+template <int D, int RF>
 void launch_d(int G, dim3 grid, hipStream_t s, const F32Args &pa) {
     const dim3 block(64 * kF32Waves);
     switch (G) {
@@ -392,10 +417,10 @@ hipError_t launch_prefill_f32(const AttnArgs &a, const int32_t *items, int32_t n
     if (wgs > INT32_MAX) return hipErrorInvalidValue;
     const F32Args pa{a, items};
     const dim3 grid((unsigned)wgs);
-    if (rope_form(a.g))
-        a.g.d == 128 ? launch_d<128, true>(G, grid, s, pa) : launch_d<64, true>(G, grid, s, pa);
-    else
-        a.g.d == 128 ? launch_d<128, false>(G, grid, s, pa) : launch_d<64, false>(G, grid, s, pa);
+    with_form(a.g, [&](auto rf) {
+        constexpr int RF = decltype(rf)::value;
+        a.g.d == 128 ? launch_d<128, RF>(G, grid, s, pa) : launch_d<64, RF>(G, grid, s, pa);
+    });
     return hipGetLastError();
 }
 
