@@ -239,6 +239,55 @@ typedef struct {
  * weights that are set when they are replayed.  The weights are copied. */
 mtn_status mtn_pool_set_qk_norm(mtn_pool *pool, const mtn_qk_norm_config *norm);
 
+/*
+ * Linear-attention layers beside the windowed ones (hybrid models; the other way to
+ * bound what a session keeps, Metronome §4.1).  A linear layer keeps one matrix S of
+ * value dims by key dims in fp32 per session and KV head, shared by the G = Hq / Hkv
+ * query heads of the KV head.  Token t of a session takes
+ *   S_t = exp(log_decay) S_(t-1) + v_t k_t^T,    out_t = scale * S_t q_t
+ * with S = 0 before a session's first token; q and k are taken as they are (neither
+ * normed nor rotated).  Products and sums are fp32 (bf16 scores and states that
+ * only make a bf16 output count to 16 bits), outputs are rounded once, states
+ * never.  Elements that are not finite reach the outputs and states of their own and
+ * later tokens of the session, where an infinity may read NaN, and no others.
+ *
+ * States: caller-owned device memory, [max_sessions][2][n_layers][n_kv_heads][D][D]
+ * fp32, last index the key dim; not initialised by the library.  One of a session's two
+ * slots holds its committed state (mtn_session_state_slot); a plan reads that one
+ * and writes the other, and its commit makes the other one the session's, so an
+ * abandoned plan leaves the state whole, and a captured mtn_attend_linear may be
+ * replayed while its plan is open.  The caller may read and change a committed state
+ * of a session with tokens between plans.
+ */
+typedef struct {
+    int32_t n_layers;         /* 1 .. 4096, beside the pool's own layers        */
+    int32_t n_q_heads;        /* up to 4096                                     */
+    int32_t n_kv_heads;       /* n_q_heads / n_kv_heads: 1, 2, 4 or 8           */
+    int32_t head_dim;         /* D of keys and values: 64 or 128                */
+    int32_t io_dtype;         /* of q, k, v and out: MTN_F32 or MTN_BF16        */
+    float   scale;            /* >= 0; 0 selects 1/sqrt(head_dim)               */
+    const float *log_decay;   /* host [n_layers][n_kv_heads], finite, <= 0      */
+} mtn_linear_config;
+
+mtn_status mtn_linear_required_bytes(const mtn_pool *pool, const mtn_linear_config *cfg, size_t *bytes);
+
+/* Give a pool linear layers (cfg NULL: take them away), while no open session holds
+ * tokens and no plan is open (MTN_ERR_BAD_STATE otherwise, or while the previous
+ * plan's stream is being captured).  states_dev: device, 256-byte aligned, >=
+ * mtn_linear_required_bytes, kept alive until the layers are taken away or the pool is
+ * destroyed (host-only pools: may be NULL).  Allocates the segments' workspace (4 D^2
+ * floats per compute unit; 67 MB on 256 at D = 128) and synchronises the stream of
+ * the previous plan.  Every plan then has to bring every linear layer too
+ * (mtn_plan_commit: MTN_ERR_BAD_STATE otherwise), mtn_session_fork copies the state,
+ * and mtn_frame_step, whose batch has no place for linear rows, is refused
+ * (MTN_ERR_BAD_STATE).  Errors: MTN_ERR_INVALID_ARG, MTN_ERR_UNSUPPORTED,
+ * MTN_ERR_DEVICE; nothing is changed. */
+mtn_status mtn_pool_set_linear(mtn_pool *pool, const mtn_linear_config *cfg, void *states_dev, size_t bytes);
+
+/* Which of an open session's two state slots, 0 or 1, is the committed one (of a
+ * session without tokens: the one that its first plan does not write). */
+mtn_status mtn_session_state_slot(const mtn_pool *pool, int32_t sid, int32_t *slot);
+
 /* Open a session: lowest free session id.  Windowed pools reserve the
  * session's whole bounded footprint, ceil(S/16) sink blocks plus R/16 ring
  * blocks with R = roundup(W + max_chunk - 1, 16), and fail with
@@ -305,7 +354,7 @@ mtn_status mtn_plan_begin(mtn_pool *pool, int32_t n_seq, const int32_t *sids /*h
                           const int32_t *n_tok /*host*/, void *stream);
 
 /* Advance every planned session by its n_tok.  MTN_ERR_BAD_STATE unless every
- * layer was appended (host-only pools excepted).  Positions that leave the window are evicted logically
+ * layer was appended and every linear layer attended (host-only pools excepted).  Positions that leave the window are evicted logically
  * (their slots become reusable); nothing is moved.                            */
 mtn_status mtn_plan_commit(mtn_pool *pool);
 
@@ -393,6 +442,16 @@ mtn_status mtn_attend_decode_append(mtn_pool *pool, int32_t layer, const void *k
                                     void *stream);
 
 /*
+ * One linear layer of the open plan, chunk or single tokens: advances every planned
+ * session's state by its tokens and writes their outputs.  q, out: device [T][Hq][D],
+ * k, v: [T][Hkv][D] in the linear layers' io_dtype and sizes, packed like k/v of
+ * mtn_frame_append_kv; out overlaps none of the others.  Once per layer and plan
+ * (MTN_ERR_BAD_STATE), in any order with the windowed layers.  Allocates nothing.
+ */
+mtn_status mtn_attend_linear(mtn_pool *pool, int32_t layer, const void *q, const void *k, const void *v,
+                             void *out, void *stream);
+
+/*
  * One whole frame for a batch of sessions (§2 task model): plan the chunk,
  * then for each layer append + chunk-prefill attend, commit; then for each
  * decode round j (only sessions with n_decode[i] > j) plan one token, for each
@@ -463,8 +522,9 @@ mtn_status mtn_plan_info(const mtn_pool *pool, int64_t *pos, int32_t *block, int
 /* Debug: write NaN into every slot that no query may read: all unassigned
  * blocks, sink-block slots at or past S, and ring slots of positions outside
  * each open session's retained set (int8 pools: codes of +127 there, NaN scales in
- * blocks without a live slot, NaN in unused rows of the tails).  Attention
- * results must not change.                                                    */
+ * blocks without a live slot, NaN in unused rows of the tails), and into every
+ * state slot of the linear layers but the committed ones of sessions with tokens.
+ * Attention results must not change.                                          */
 mtn_status mtn_debug_poison_dead(mtn_pool *pool, void *stream);
 
 /* Tuning: query rows per chunk-prefill pass (rows are token x G + group head;
@@ -507,6 +567,9 @@ mtn_status mtn_debug_inject_failure(mtn_pool *pool, int64_t launch_index);
  * prefill's time as the rest of the class does to the decode's.               */
 mtn_status mtn_pool_set_timing(mtn_pool *pool, int32_t enable);
 mtn_status mtn_pool_kernel_times(mtn_pool *pool, int64_t *launches, double *ms);
+/* ... the launches and milliseconds of mtn_attend_linear in that call (a segmented
+ * chunk's three launches count as one).                                       */
+mtn_status mtn_pool_linear_times(const mtn_pool *pool, int64_t *launches, double *ms);
 mtn_status mtn_pool_prefill_merge_times(const mtn_pool *pool, int64_t *launches, double *ms);
 
 /* Plain device copy (dst = src, `bytes` a multiple of 16, both 16-byte

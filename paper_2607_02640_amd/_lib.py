@@ -46,7 +46,8 @@ EXPORTS = [
     "mtn_pool_required_bytes", "mtn_pool_create", "mtn_pool_destroy",
     "mtn_session_open", "mtn_session_close", "mtn_plan_begin", "mtn_plan_commit",
     "mtn_plan_abort",
-    "mtn_pool_set_rope", "mtn_pool_set_qk_norm", "mtn_session_fork", "mtn_pool_resize",
+    "mtn_pool_set_rope", "mtn_pool_set_qk_norm", "mtn_linear_required_bytes",
+    "mtn_pool_set_linear", "mtn_session_state_slot", "mtn_attend_linear", "mtn_pool_linear_times", "mtn_session_fork", "mtn_pool_resize",
     "mtn_frame_append_kv", "mtn_attend_chunk_prefill", "mtn_attend_decode",
     "mtn_attend_decode_append", "mtn_attend_decode_noalloc",
     "mtn_frame_step", "mtn_pool_stats", "mtn_session_info", "mtn_session_block_table",
@@ -79,6 +80,14 @@ class RopeConfig(C.Structure):
 
 class QkNormConfig(C.Structure):
     _fields_ = [("q_weight", C.POINTER(C.c_float)), ("k_weight", C.POINTER(C.c_float)), ("eps", C.c_double)]
+
+
+class LinearConfig(C.Structure):
+    _fields_ = [
+        ("n_layers", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+        ("head_dim", C.c_int32), ("io_dtype", C.c_int32), ("scale", C.c_float),
+        ("log_decay", C.POINTER(C.c_float)),
+    ]
 
 
 class PoolStats(C.Structure):
@@ -139,6 +148,11 @@ def load() -> C.CDLL:
         "mtn_pool_destroy": (None, [vp]),
         "mtn_pool_set_rope": (i32, [vp, C.POINTER(RopeConfig)]),
         "mtn_pool_set_qk_norm": (i32, [vp, C.POINTER(QkNormConfig)]),
+        "mtn_linear_required_bytes": (i32, [vp, C.POINTER(LinearConfig), C.POINTER(C.c_size_t)]),
+        "mtn_pool_set_linear": (i32, [vp, C.POINTER(LinearConfig), vp, C.c_size_t]),
+        "mtn_session_state_slot": (i32, [vp, i32, P32]),
+        "mtn_attend_linear": (i32, [vp, i32, vp, vp, vp, vp, vp]),
+        "mtn_pool_linear_times": (i32, [vp, P64, C.POINTER(C.c_double)]),
         "mtn_session_fork": (i32, [vp, i32, i32, P32, vp]),
         "mtn_pool_resize": (i32, [vp, i64, vp, C.c_size_t, vp]),
         "mtn_session_open": (i32, [vp, P32]),
@@ -247,6 +261,7 @@ class Pool:
                     "required_bytes")
         self.required_bytes = nbytes.value
         self.kv = kv
+        self.states = None  # of the linear layers: set_linear
         h = C.c_void_p()
         st = self.lib.mtn_pool_create(C.byref(self.cfg), _ptr(kv) if kv is not None else None,
                                       C.c_size_t(kv.numel() * kv.element_size() if kv is not None else 0),
@@ -363,6 +378,56 @@ class Pool:
         self._not_captured("clear_qk_norm")
         self._check(self.lib.mtn_pool_set_qk_norm(self.h, None), "clear_qk_norm")
 
+    @staticmethod
+    def linear_shape(max_sessions, n_layers, n_kv_heads, head_dim) -> tuple:
+        """Shape of the float32 tensor that holds the linear layers' states."""
+        return (max_sessions, 2, n_layers, n_kv_heads, head_dim, head_dim)
+
+    def set_linear(self, *, n_layers, n_q_heads, n_kv_heads, head_dim, log_decay, states=None, dtype="bf16",
+                   scale=0.0) -> None:
+        """Linear-attention layers beside the pool's own (mtn_pool_set_linear).
+        ``log_decay``: [n_layers][n_kv_heads], a tensor, an array or lists;
+        ``states``: a contiguous float32 device tensor of ``linear_shape``, which the
+        pool then holds (host-only pools: None)."""
+        where = "set_linear"
+        self._not_captured(where)
+        if dtype not in ("f32", "bf16"):
+            raise MtnError(MTN_ERR_UNSUPPORTED, where, f"dtype {dtype}")
+        if states is not None and not self.host_only:
+            import torch
+            shape = self.linear_shape(self.cfg.max_sessions, n_layers, n_kv_heads, head_dim)
+            if tuple(states.shape) != shape or states.dtype != torch.float32 or not states.is_contiguous() \
+                    or states.device != self.kv.device:
+                raise MtnError(MTN_ERR_INVALID_ARG, where, f"states: not a contiguous float32 tensor {shape} on the "
+                               "pool's device")
+        decay = _host_floats(log_decay, where, max(n_layers, 0) * max(n_kv_heads, 0))
+        cfg = LinearConfig(n_layers, n_q_heads, n_kv_heads, head_dim, DTYPES[dtype][1], scale,
+                           C.cast(decay, C.POINTER(C.c_float)))
+        size = C.c_size_t(states.numel() * states.element_size() if states is not None else 0)
+        self._check(self.lib.mtn_pool_set_linear(self.h, C.byref(cfg), _ptr(states), size), where)
+        self.states = states
+
+    def clear_linear(self) -> None:
+        """Take the linear layers away; the pool then holds their states no longer."""
+        self._not_captured("clear_linear")
+        self._check(self.lib.mtn_pool_set_linear(self.h, None, None, C.c_size_t(0)), "clear_linear")
+        self.states = None
+
+    def state_slot(self, sid: int) -> int:
+        """Which of session ``sid``'s two slots of the states is the committed one."""
+        slot = C.c_int32()
+        self._check(self.lib.mtn_session_state_slot(self.h, sid, C.byref(slot)), "state_slot")
+        return slot.value
+
+    def session_state(self, sid: int):
+        """The committed state of session ``sid``: a view [layers][KV heads][D][D] of
+        the states (undefined while the session has no tokens)."""
+        return self.states[sid, self.state_slot(sid)]
+
+    def attend_linear(self, layer, q, k, v, out, stream=None) -> None:
+        self._check(self.lib.mtn_attend_linear(self.h, layer, _ptr(q), _ptr(k), _ptr(v), _ptr(out),
+                                               _stream(stream)), "attend_linear")
+
     def set_decode_kernel(self, kind: int) -> None:
         """0 = by shape, 1 = vector kernel, 2 = matrix-core kernel."""
         self._check(self.lib.mtn_pool_set_decode_kernel(self.h, kind), "set_decode_kernel")
@@ -463,6 +528,8 @@ class Pool:
         # the chunk prefill's share of the merges
         self._check(self.lib.mtn_pool_prefill_merge_times(self.h, n, ms), "kernel_times")
         times["prefill_merge"] = (n[0], ms[0])
+        self._check(self.lib.mtn_pool_linear_times(self.h, n, ms), "kernel_times")
+        times["linear"] = (n[0], ms[0])
         return times
 
 

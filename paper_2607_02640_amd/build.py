@@ -24,17 +24,18 @@ COMMON = [
 ]
 
 SOURCES = ["mtn_host.cpp", "mtn_admission.cpp", "mtn_kernels.hip", "mtn_mfma.hip",
-           "mtn_prefill_f32.hip", "mtn_i8.hip", "mtn_pages.hip"]
+           "mtn_prefill_f32.hip", "mtn_i8.hip", "mtn_pages.hip", "mtn_linear.hip"]
 
 # Per-source code generation.  The matrix-core decode takes its MFMA
 # accumulators in ordinary VGPRs: in the AGPR form the compiler copied the 32
 # output accumulators out of and back into AGPRs around every block's rescale
 # test (about 100 of its 250 vector instructions per block; measured 1.3 %
 # faster fp8 and 0.4 % faster bf16 launches without them).
-# The int8 decode and the fp32 prefill take the same form.
+# The int8 decode, the fp32 prefill and the linear layers take the same form.
 EXTRA = {"mtn_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "mtn_i8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-         "mtn_prefill_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+         "mtn_prefill_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "mtn_linear.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def compile_flags(src: str) -> list:

@@ -8,6 +8,7 @@
 // decodes single tokens, for all due sessions in one batch.
 #include "mtn.h"
 #include "mtn_kernels.h"
+#include "mtn_linear.h"
 
 #include <hip/hip_runtime.h>
 
@@ -38,8 +39,11 @@ constexpr int kPfMaxSplit = 16;  // ... and key segments of a pass, at most
 // launch for the host, too)
 constexpr int kPfMinBlocksF32 = 2;
 constexpr double kPfMinSavedF32 = 3.0;
-// timing classes: append, prefill, decode, the decode's merge, the prefill's merge
-constexpr int kTimeClasses = 5;
+// timing classes: append, prefill, decode, the decode's merge, the prefill's merge,
+// the linear layers
+constexpr int kTimeClasses = 6;
+// segments' states that a pool with linear layers has room for, per compute unit
+constexpr int kLinSegUnits = 4;
 constexpr size_t kZeroPage = 2 * kBlock * 128 * 4;  // 16 KiB
 
 // Lowest-free-first block allocator over a bitmap (bit set = free).
@@ -124,7 +128,23 @@ struct mtn_pool {
     std::vector<int32_t> run_tok0, run_len;  // append runs: consecutive slots of one block
     std::vector<uint8_t> layer_done;
 
+    // linear layers (n_layers 0: none)
+    mtn_linear_config lin = {};
+    std::vector<uint8_t> lin_slot;    // which of a session's two states is committed
+    std::vector<uint8_t> lin_done;    // layers of the open plan
+    std::vector<int32_t> lin_items;   // ... kLinItem words per sequence or segment
+    bool lin_split = false;           // ... some sequence is cut into segments
+    int32_t lin_max = 0;              // ... tokens of the longest item
+    float *lin_states = nullptr;      // caller's
+    float *d_lin_decay = nullptr;     // [n_layers][n_kv_heads] log2
+    float *d_lin_seg = nullptr;       // segments' states
+    int64_t lin_seg_cap = 0;          // ... of so many (segment, KV head) pairs
+    int32_t *d_lin_items = nullptr;   // in d_meta
+    int64_t lin_launch = 0;           // launches and milliseconds that
+    double lin_ms = 0.0;              // mtn_pool_kernel_times last found
+
     // device
+    int device = 0;                // the pool's
     int32_t max_tok = 0;           // capacity of one plan in tokens
     int32_t *d_table = nullptr;
     int32_t *d_meta = nullptr;     // packed plan metadata
@@ -633,6 +653,45 @@ mtn_status fork_pages(mtn_pool *P, int32_t src, const std::vector<int32_t> &sids
     return copy_tails(P, tails(P), tails(P), tail_slots, s);
 }
 
+// Words of one session's state slot (every linear layer), and of both.
+int64_t lin_slot_floats(const mtn_linear_config &c) {
+    return (int64_t)c.n_layers * c.n_kv_heads * c.head_dim * c.head_dim;
+}
+
+// The linear layers' work: one item per sequence, or, where those leave compute
+// units idle, per segment of one (each finds its own state from zero, a scan
+// then gives each the state before it).
+void plan_linear(mtn_pool *P) {
+    P->lin_items.clear();
+    P->lin_split = false;
+    P->lin_max = 0;
+    if (!P->lin.n_layers) return;
+    const int64_t hkv = P->lin.n_kv_heads;
+    int64_t len = P->max_ntok;  // tokens of a segment
+    if (!P->all_single && P->n_cu > 0 && P->n_seq * hkv < P->n_cu) {
+        const int64_t want = std::max<int64_t>(2 * P->n_cu / hkv, 1);  // segments
+        len = std::max<int64_t>(ceil_div(ceil_div(P->T, want), kLinTile) * kLinTile, 2 * kLinTile);
+        auto segments = [&] {
+            int64_t m = 0;
+            for (int32_t i = 0; i < P->n_seq; ++i) m += ceil_div(P->seq_ntok[i], len);
+            return m;
+        };
+        while (segments() * hkv > P->lin_seg_cap || segments() > P->n_seq + kLinMaxSeg) len += kLinTile;
+    }
+    for (int32_t i = 0; i < P->n_seq; ++i) {
+        const int32_t sid = P->seq_sid[i], nt = P->seq_ntok[i];
+        const int32_t nseg = (int32_t)ceil_div(nt, len);
+        const int32_t slot = 2 * sid + P->lin_slot[sid] + (P->seq_pos0[i] == 0 ? kLinFresh : 0);
+        for (int32_t j = 0; j < nseg; ++j) {
+            const int32_t n = (int32_t)std::min<int64_t>(len, nt - j * len);
+            const int32_t rec[kLinItem] = {P->tok_row[P->seq_first[i]] + (int32_t)(j * len), n, slot, j | nseg << 16};
+            P->lin_items.insert(P->lin_items.end(), rec, rec + kLinItem);
+            P->lin_max = std::max(P->lin_max, n);
+        }
+        P->lin_split = P->lin_split || nseg > 1;
+    }
+}
+
 // Internal plan begin.  rows == nullptr packs io rows in plan order.
 mtn_status plan_begin(mtn_pool *P, int32_t n_seq, const int32_t *sids, const int32_t *n_tok,
                       const int32_t *rows, void *stream) {
@@ -733,7 +792,9 @@ mtn_status plan_begin(mtn_pool *P, int32_t n_seq, const int32_t *sids, const int
     // one-token plans never reach the chunk prefill
     P->pf_items.clear();
     if (!P->all_single) plan_prefill(P);
+    plan_linear(P);
     P->layer_done.assign((size_t)P->cfg.n_layers, 0);
+    P->lin_done.assign((size_t)P->lin.n_layers, 0);
     P->plan_open = true;
     P->plan_stream = stream;
     if (P->host_only) return MTN_OK;
@@ -742,7 +803,8 @@ mtn_status plan_begin(mtn_pool *P, int32_t n_seq, const int32_t *sids, const int
     // takes a small blob from host memory itself
     const int32_t U = (int32_t)P->upd_idx.size();
     const int32_t NR = (int32_t)P->run_tok0.size();
-    const size_t o_items = ((size_t)5 * T + 2 * U + kPfItem - 1) / kPfItem * kPfItem;  // records 32-byte aligned
+    const size_t NL = P->lin_items.size();  // (linear layers' items behind the token fields)
+    const size_t o_items = ((size_t)5 * T + NL + 2 * U + kPfItem - 1) / kPfItem * kPfItem;  // records 32-byte aligned
     const size_t words = o_items + P->pf_items.size() + 2 * (size_t)NR;
     const bool small = words <= (size_t)kSmallWords;
     // a failed upload abandons the plan: the pool is as before the call
@@ -778,6 +840,7 @@ mtn_status plan_begin(mtn_pool *P, int32_t n_seq, const int32_t *sids, const int
                 h[o - T + tt] |= slot << 8;
             }
         }
+    put(P->lin_items.data(), (int32_t)NL);
     put(P->upd_idx.data(), U);
     put(P->upd_val.data(), U);
     while (o < o_items) h[o++] = 0;
@@ -798,11 +861,12 @@ mtn_status plan_begin(mtn_pool *P, int32_t n_seq, const int32_t *sids, const int
     P->view.tok_off = d + 4 * T;
     P->view.rope = P->d_rope;
     P->view.n_tok = (int32_t)T;
+    P->d_lin_items = d + 5 * T;
     P->d_pf_items = d + o_items;
     P->d_run_tok0 = P->d_pf_items + P->pf_items.size();
     P->d_run_len = P->d_run_tok0 + NR;
     const int32_t *from = small ? h : d;  // what the plan kernel reads
-    he = launch_plan_apply(small ? h : nullptr, d, (int32_t)o, from + 5 * T, from + 5 * T + U, U,
+    he = launch_plan_apply(small ? h : nullptr, d, (int32_t)o, from + 5 * T + NL, from + 5 * T + NL + U, U,
                            P->d_table, from + T, (int32_t)T, P->d_inv_freq, P->cfg.head_dim / 2,
                            P->d_rope, s);
     if (he != hipSuccess) return upload_fail(he, "launch_plan_apply");
@@ -829,9 +893,13 @@ mtn_status plan_commit(mtn_pool *P) {
     if (!P->host_only)
         for (auto d : P->layer_done)
             if (!d) return fail(P, MTN_ERR_BAD_STATE, "commit before every layer was appended");
+    if (!P->host_only)
+        for (auto d : P->lin_done)
+            if (!d) return fail(P, MTN_ERR_BAD_STATE, "commit before every linear layer was attended");
     for (int32_t i = 0; i < P->n_seq; ++i) {
         P->len[P->seq_sid[i]] += P->seq_ntok[i];
         P->tail[P->seq_sid[i]] = P->seq_tail[i];
+        if (P->lin.n_layers) P->lin_slot[P->seq_sid[i]] ^= 1;
     }
     P->plan_open = false;
     return MTN_OK;
@@ -971,12 +1039,22 @@ mtn_status upload_tables(mtn_pool *P, std::initializer_list<Upload> ups, const c
     return e == hipSuccess ? MTN_OK : hip_fail(P, e, what);
 }
 
-mtn_status check_call(mtn_pool *P, int32_t layer, void *stream) {
+mtn_status check_linear(const mtn_linear_config &c) {
+    if (c.n_layers < 1 || c.n_q_heads < 1 || c.n_kv_heads < 1 || c.n_q_heads % c.n_kv_heads) return MTN_ERR_INVALID_ARG;
+    if (c.n_layers > 4096 || c.n_q_heads > 4096) return MTN_ERR_UNSUPPORTED;  // (sizes of 64 bits stay far off)
+    if (c.io_dtype != MTN_F32 && c.io_dtype != MTN_BF16) return MTN_ERR_UNSUPPORTED;
+    if (!linear_supported(c.io_dtype, c.head_dim, c.n_q_heads / c.n_kv_heads)) return MTN_ERR_UNSUPPORTED;
+    if (!std::isfinite(c.scale) || c.scale < 0.f) return MTN_ERR_INVALID_ARG;
+    return MTN_OK;
+}
+
+mtn_status check_call(mtn_pool *P, int32_t layer, void *stream, bool linear = false) {
     if (!P) return MTN_ERR_INVALID_ARG;
     if (P->host_only) return fail(P, MTN_ERR_BAD_STATE, "host-only pool has no device path");
     if (!P->plan_open) return fail(P, MTN_ERR_BAD_STATE, "no open plan");
     if (stream != P->plan_stream) return fail(P, MTN_ERR_INVALID_ARG, "stream differs from plan's");
-    if (layer < 0 || layer >= P->cfg.n_layers) return fail(P, MTN_ERR_INVALID_ARG, "bad layer");
+    if (layer < 0 || layer >= (linear ? P->lin.n_layers : P->cfg.n_layers))
+        return fail(P, MTN_ERR_INVALID_ARG, "bad layer");
     return MTN_OK;
 }
 
@@ -1372,6 +1450,7 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
     P->len.assign((size_t)cfg->max_sessions, 0);
     P->n_assigned.assign((size_t)cfg->max_sessions, 0);
     P->tail.assign((size_t)cfg->max_sessions, 0);
+    P->lin_slot.assign((size_t)cfg->max_sessions, 0);
     P->alloc.reset(cfg->n_blocks);
     P->max_tok = cfg->max_sessions * cfg->max_chunk;
     // the planner's per-plan vectors at their largest, so that planning
@@ -1389,6 +1468,7 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
     P->pf_items.reserve(kPfItem * max_items);
     P->pf_order.reserve(max_items);
     P->layer_done.reserve((size_t)cfg->n_layers);
+    P->lin_items.reserve((size_t)kLinItem * ((size_t)cfg->max_sessions + kLinMaxSeg));
     if (!host_only) {
         auto bail = [&](hipError_t e, const char *w) {
             (void)e;
@@ -1402,8 +1482,10 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
                                 (hipStream_t)stream)) != hipSuccess)
             return bail(e, "table upload");
         // per plan: 5 T token fields, 2 U table updates (U <= T), kPfItem per
-        // prefill pass (aligned to a record), 2 per append run (<= T)
-        size_t meta = sizeof(int32_t) * ((size_t)P->max_tok * 9 + kPfItem * max_items + 64);
+        // prefill pass (aligned to a record), 2 per append run (<= T), the linear
+        // layers' items
+        size_t meta = sizeof(int32_t) * ((size_t)P->max_tok * 9 + kPfItem * max_items + 64 +
+                                         (size_t)kLinItem * ((size_t)cfg->max_sessions + kLinMaxSeg));
         if ((e = hipMalloc(&P->d_meta, meta)) != hipSuccess) return bail(e, "meta");
         for (int i = 0; i < kStages; ++i) {
             if ((e = hipHostMalloc(&P->h_stage[i], meta, hipHostMallocDefault)) != hipSuccess)
@@ -1434,6 +1516,7 @@ mtn_status pool_init(mtn_pool *P, const mtn_pool_config *cfg, void *kv_dev, void
             hipSuccess)
             return bail(e, "cu count");
         P->n_cu = n_cu;
+        P->device = dev;
         // zero page: at least one whole (block, head) pair, K + V^T, at the
         // largest element size and head dim
         if ((e = hipMalloc(&P->d_zero, kZeroPage)) != hipSuccess) return bail(e, "zero page");
@@ -1485,6 +1568,8 @@ void mtn_pool_destroy(mtn_pool *P) {
         (void)hipFree(P->d_table);
         (void)hipFree(P->d_meta);
         (void)hipFree(P->d_norm);
+        (void)hipFree(P->d_lin_decay);
+        (void)hipFree(P->d_lin_seg);
         (void)hipFree(P->d_inv_freq);
         (void)hipFree(P->d_part);
         (void)hipFree(P->d_zero);
@@ -1556,6 +1641,86 @@ mtn_status mtn_pool_set_qk_norm(mtn_pool *P, const mtn_qk_norm_config *cfg) {
     });
 }
 
+mtn_status mtn_linear_required_bytes(const mtn_pool *P, const mtn_linear_config *cfg, size_t *bytes) {
+    if (!P || !cfg || !bytes) return MTN_ERR_INVALID_ARG;
+    if (mtn_status st = check_linear(*cfg)) return st;
+    *bytes = 2 * sizeof(float) * (size_t)P->cfg.max_sessions * (size_t)lin_slot_floats(*cfg);
+    return MTN_OK;
+}
+
+mtn_status mtn_pool_set_linear(mtn_pool *P, const mtn_linear_config *cfg, void *states_dev, size_t bytes) {
+    return guarded(P, [&]() -> mtn_status {
+        if (!P) return MTN_ERR_INVALID_ARG;
+        if (mtn_status st = check_reform(P)) return st;
+        mtn_linear_config c = {};
+        std::vector<float> log2s;
+        if (cfg) {
+            c = *cfg;
+            size_t need = 0;
+            if (mtn_status st = mtn_linear_required_bytes(P, cfg, &need)) return fail(P, st, "bad linear config");
+            if (!P->host_only && (!states_dev || ((uintptr_t)states_dev & 255) || bytes < need))
+                return fail(P, MTN_ERR_INVALID_ARG, "null, misaligned or small state buffer");
+            if (!c.log_decay) return fail(P, MTN_ERR_INVALID_ARG, "null log_decay");
+            const size_t n = (size_t)c.n_layers * c.n_kv_heads;
+            for (size_t i = 0; i < n; ++i) {
+                if (!(c.log_decay[i] <= 0.f) || !std::isfinite(c.log_decay[i]))
+                    return fail(P, MTN_ERR_INVALID_ARG, "log_decay above 0 or not finite");
+                log2s.push_back(std::max((float)(c.log_decay[i] * 1.4426950408889634), -3.0e38f));
+            }
+            if (c.scale == 0.f) c.scale = (float)(1.0 / std::sqrt((double)c.head_dim));
+        }
+        c.log_decay = nullptr;
+        P->lin_done.reserve((size_t)c.n_layers);
+        float *decay = nullptr, *seg = nullptr;
+        int64_t cap = 0;
+        if (!P->host_only) {
+            // new buffers before the old ones go; a capture under way on another stream
+            // is left alone
+            void *const last = P->have_last_stream ? P->last_stream : nullptr;
+            if (mtn_status st = refuse_capture(P, last)) return st;
+            hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+            HIP_TRY(P, hipThreadExchangeStreamCaptureMode(&mode));
+            int dev = 0;
+            hipError_t e = hipGetDevice(&dev);
+            if (e == hipSuccess) e = hipSetDevice(P->device);
+            if (e == hipSuccess && cfg) {
+                cap = (int64_t)kLinSegUnits * P->n_cu;
+                e = hipMalloc(&decay, sizeof(float) * log2s.size());
+                if (e == hipSuccess) e = hipMalloc(&seg, sizeof(float) * (size_t)cap * c.head_dim * c.head_dim);
+                if (e == hipSuccess)
+                    e = hipMemcpyAsync(decay, log2s.data(), sizeof(float) * log2s.size(), hipMemcpyHostToDevice,
+                                       (hipStream_t)last);
+            }
+            const hipError_t e2 = hipStreamSynchronize((hipStream_t)last);
+            if (e == hipSuccess) e = e2;
+            if (e != hipSuccess) {
+                (void)hipFree(decay);
+                (void)hipFree(seg);
+            } else {
+                (void)hipFree(P->d_lin_decay);
+                (void)hipFree(P->d_lin_seg);
+            }
+            (void)hipSetDevice(dev);
+            (void)hipThreadExchangeStreamCaptureMode(&mode);
+            if (e != hipSuccess) return hip_fail(P, e, "linear layers' buffers");
+        }
+        P->lin = c;
+        P->lin_states = cfg ? (float *)states_dev : nullptr;
+        P->d_lin_decay = decay;
+        P->d_lin_seg = seg;
+        P->lin_seg_cap = cap;
+        return MTN_OK;
+    });
+}
+
+mtn_status mtn_session_state_slot(const mtn_pool *P, int32_t sid, int32_t *slot) {
+    if (!P || !slot) return MTN_ERR_INVALID_ARG;
+    if (sid < 0 || sid >= P->cfg.max_sessions || !P->is_open[sid]) return MTN_ERR_BAD_SESSION;
+    if (!P->lin.n_layers) return MTN_ERR_BAD_STATE;
+    *slot = P->lin_slot[sid];
+    return MTN_OK;
+}
+
 mtn_status mtn_session_open(mtn_pool *P, int32_t *sid_out) {
     return guarded(P, [&]() -> mtn_status {
         if (!P || !sid_out) return MTN_ERR_INVALID_ARG;
@@ -1575,6 +1740,7 @@ mtn_status mtn_session_open(mtn_pool *P, int32_t *sid_out) {
         P->len[sid] = 0;
         P->n_assigned[sid] = 0;
         P->tail[sid] = 0;
+        P->lin_slot[sid] = 0;
         P->n_open++;
         *sid_out = sid;
         return MTN_OK;
@@ -1631,6 +1797,10 @@ mtn_status mtn_session_fork(mtn_pool *P, int32_t sid, int32_t n_copies, int32_t 
         if (P->int8 && open_rows(P, P->len[sid]))
             for (const int32_t c : sids)
                 tail_slots.emplace_back(2 * sid + P->tail[sid], 2 * c + P->tail[sid]);
+        std::vector<std::pair<int32_t, int32_t>> states;  // of the linear layers
+        if (P->lin.n_layers && P->len[sid])
+            for (const int32_t c : sids)
+                states.emplace_back(2 * sid + P->lin_slot[sid], 2 * c + P->lin_slot[sid]);
         mtn_status st = launch_gate(P);
         if (!st) st = follow_last_stream(P, stream);
         if (st) return st;
@@ -1641,6 +1811,8 @@ mtn_status mtn_session_fork(mtn_pool *P, int32_t sid, int32_t n_copies, int32_t 
         }
         if (pages) {
             st = fork_pages(P, sid, sids, tail_slots, (hipStream_t)stream);
+            const TailView lin{(uint8_t *)P->lin_states, (int64_t)sizeof(float) * lin_slot_floats(P->lin)};
+            if (!st) st = copy_tails(P, lin, lin, states, (hipStream_t)stream);
             if (st) {  // the blocks go back; what a launch wrote lies in free blocks
                 for (const int32_t c : sids) {
                     int32_t *row = &P->table[(size_t)c * P->row_len];
@@ -1658,6 +1830,7 @@ mtn_status mtn_session_fork(mtn_pool *P, int32_t sid, int32_t n_copies, int32_t 
             P->len[c] = P->len[sid];
             P->n_assigned[c] = (int32_t)pages;
             P->tail[c] = P->tail[sid];
+            P->lin_slot[c] = P->lin_slot[sid];
         }
         P->n_open += n_copies;
         P->assigned += pages * n_copies;
@@ -1853,10 +2026,50 @@ mtn_status mtn_attend_decode_noalloc(mtn_pool *P, int32_t layer, const void *q, 
     });
 }
 
+mtn_status mtn_attend_linear(mtn_pool *P, int32_t layer, const void *q, const void *k, const void *v, void *out,
+                             void *stream) {
+    return guarded(P, [&]() -> mtn_status {
+        mtn_status st = check_call(P, layer, stream, true);
+        if (st) return st;
+        if (bad_buf(q) || bad_buf(k) || bad_buf(v) || bad_buf(out))
+            return fail(P, MTN_ERR_INVALID_ARG, "null or misaligned q, k, v or out");
+        if (P->lin_done[layer]) return fail(P, MTN_ERR_BAD_STATE, "linear layer already attended");
+        if ((st = launch_gate(P))) return st;
+        const mtn_linear_config &c = P->lin;
+        const int64_t per = (int64_t)c.n_kv_heads * c.head_dim * c.head_dim;
+        LinArgs a;
+        a.items = P->d_lin_items;
+        a.q = q;
+        a.k = k;
+        a.v = v;
+        a.out = out;
+        a.state = P->lin_states + layer * per;
+        a.slot_stride = c.n_layers * per;
+        a.seg = P->d_lin_seg;
+        a.log2_decay = P->d_lin_decay + (size_t)layer * c.n_kv_heads;
+        a.scale = c.scale;
+        a.hq = c.n_q_heads;
+        a.hkv = c.n_kv_heads;
+        a.d = c.head_dim;
+        a.n_items = (int32_t)(P->lin_items.size() / kLinItem);
+        hipStream_t s = (hipStream_t)stream;
+        hipEvent_t e0;
+        if ((st = timing_begin(P, s, &e0))) return st;
+        if (P->all_single)
+            HIP_TRY(P, launch_linear_decode(c.io_dtype, a, P->n_cu, s));
+        else
+            HIP_TRY(P, launch_linear_chunk(c.io_dtype, a, P->lin_max, P->lin_split, s));
+        if ((st = timing_end(P, 5, e0, s))) return st;
+        P->lin_done[layer] = 1;
+        return MTN_OK;
+    });
+}
+
 mtn_status mtn_frame_step(mtn_pool *P, const mtn_frame_batch *b, void *stream) {
     return guarded(P, [&]() -> mtn_status {
         if (!P || !b) return MTN_ERR_INVALID_ARG;
         if (P->plan_open) return fail(P, MTN_ERR_BAD_STATE, "a plan is already open");
+        if (P->lin.n_layers) return fail(P, MTN_ERR_BAD_STATE, "a pool with linear layers takes the per-layer calls");
         const int32_t n = b->n_seq;
         if (n < 1 || n > P->cfg.max_sessions || !b->sids || !b->chunk_len || !b->n_decode)
             return fail(P, MTN_ERR_INVALID_ARG, "bad batch");
@@ -1989,7 +2202,12 @@ mtn_status mtn_debug_poison_dead(mtn_pool *P, void *stream) {
         hipStream_t s = (hipStream_t)stream;
         uint16_t *d_live = nullptr;
         const size_t live_bytes = sizeof(uint16_t) * live.size();
-        HIP_TRY(P, hipMalloc(&d_live, live_bytes + rows.size()));
+        // ... state slots: all but the committed one of a session with tokens
+        std::vector<uint8_t> dead(P->lin.n_layers ? 2 * (size_t)P->cfg.max_sessions : 0, 1);
+        if (!dead.empty())
+            for (int32_t sid = 0; sid < P->cfg.max_sessions; ++sid)
+                if (P->is_open[sid] && P->len[sid]) dead[2 * sid + P->lin_slot[sid]] = 0;
+        HIP_TRY(P, hipMalloc(&d_live, live_bytes + rows.size() + dead.size()));
         HIP_TRY(P, hipMemcpy(d_live, live.data(), live_bytes, hipMemcpyHostToDevice));
         uint8_t *d_rows = (uint8_t *)d_live + live_bytes;
         if (P->int8) HIP_TRY(P, hipMemcpy(d_rows, rows.data(), rows.size(), hipMemcpyHostToDevice));
@@ -2000,6 +2218,11 @@ mtn_status mtn_debug_poison_dead(mtn_pool *P, void *stream) {
                                         (int32_t)rows.size(), d_live, d_rows, s));
         else
             HIP_TRY(P, launch_poison(P->cfg.kv_dtype, geom(P), P->cfg.n_layers, P->cfg.n_blocks, d_live, s));
+        if (!dead.empty()) {
+            HIP_TRY(P, hipMemcpy(d_rows + rows.size(), dead.data(), dead.size(), hipMemcpyHostToDevice));
+            HIP_TRY(P, launch_linear_poison(P->lin_states, lin_slot_floats(P->lin), (int32_t)dead.size(),
+                                            d_rows + rows.size(), s));
+        }
         HIP_TRY(P, hipStreamSynchronize(s));
         HIP_TRY(P, hipFree(d_live));
         return MTN_OK;
@@ -2074,6 +2297,8 @@ mtn_status mtn_pool_kernel_times(mtn_pool *P, int64_t *launches, double *ms) {
         }
         launches[3] += P->pf_merge_launch = P->t_launch[4];
         ms[3] += P->pf_merge_ms = P->t_ms[4];
+        P->lin_launch = P->t_launch[5];
+        P->lin_ms = P->t_ms[5];
         std::fill_n(P->t_launch, kTimeClasses, 0);
         std::fill_n(P->t_ms, kTimeClasses, 0.0);
         return MTN_OK;
@@ -2084,6 +2309,13 @@ mtn_status mtn_pool_prefill_merge_times(const mtn_pool *P, int64_t *launches, do
     if (!P || !launches || !ms) return MTN_ERR_INVALID_ARG;
     *launches = P->pf_merge_launch;
     *ms = P->pf_merge_ms;
+    return MTN_OK;
+}
+
+mtn_status mtn_pool_linear_times(const mtn_pool *P, int64_t *launches, double *ms) {
+    if (!P || !launches || !ms) return MTN_ERR_INVALID_ARG;
+    *launches = P->lin_launch;
+    *ms = P->lin_ms;
     return MTN_OK;
 }
 

@@ -5,6 +5,7 @@
 // host-only pools, which never launch.  Every launch here fails with
 // hipErrorNotSupported; the shape queries answer as the kernels do.
 #include "mtn_kernels.h"
+#include "mtn_linear.h"
 
 namespace mtn {
 
@@ -77,5 +78,9 @@ bool prefill_mfma_supported(int dtype, int d, int g) {
     return (((dtype == 0 || dtype == 1 || dtype == 3) && (d == 128 || d == 64)) || (dtype == 2 && d == 128)) &&
            group_ok(g);
 }
+bool linear_supported(int dtype, int d, int g) { return (dtype == 0 || dtype == 1) && (d == 64 || d == 128) && group_ok(g); }
+hipError_t launch_linear_decode(int, const LinArgs &, int, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_linear_chunk(int, const LinArgs &, int, bool, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_linear_poison(float *, int64_t, int32_t, const uint8_t *, hipStream_t) { return hipErrorNotSupported; }
 
 }  // namespace mtn

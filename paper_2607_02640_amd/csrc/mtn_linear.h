@@ -1,0 +1,38 @@
+// Internal launch interface of the linear-attention layers (mtn_linear.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace mtn {
+
+// One sequence of a plan, or one segment of it: {first io row, tokens, state slot
+// (2 * session + which of its two), with kLinFresh where the session holds no
+// token yet, segment | segments << 16}.  A sequence's segments follow one another;
+// all but its last hold a multiple of kLinTile tokens.
+constexpr int kLinItem = 4;
+constexpr int32_t kLinFresh = 1 << 30;
+constexpr int kLinTile = 64;
+constexpr int kLinMaxSeg = 1024;  // segments of a plan that cuts sequences, at most
+
+struct LinArgs {
+    const int32_t *items;     // device [n_items][kLinItem]
+    const void *q, *k, *v;    // [rows][Hq | Hkv | Hkv][D]
+    void *out;                // [rows][Hq][D]
+    float *state;             // the layer's states in slot 0: [Hkv][value D][key D]
+    int64_t slot_stride;      // floats from a slot to the next
+    float *seg;               // segments' states [item][Hkv][D][D]
+    const float *log2_decay;  // device [Hkv]
+    float scale;
+    int32_t hq, hkv, d, n_items;
+};
+
+bool linear_supported(int dtype, int d, int g);
+// Plans of one token per sequence
+hipError_t launch_linear_decode(int dtype, const LinArgs &a, int n_cu, hipStream_t s);
+// Plans of any lengths; max_tok: the longest item, split: some sequence has segments
+hipError_t launch_linear_chunk(int dtype, const LinArgs &a, int max_tok, bool split, hipStream_t s);
+// Debug: NaN into every state slot with dead[slot] != 0 (slots of slot_stride floats)
+hipError_t launch_linear_poison(float *states, int64_t slot_stride, int32_t n_slots, const uint8_t *dead,
+                                hipStream_t s);
+
+}  // namespace mtn
