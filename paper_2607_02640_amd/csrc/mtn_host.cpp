@@ -669,7 +669,12 @@ void plan_linear(mtn_pool *P) {
     const int64_t hkv = P->lin.n_kv_heads;
     int64_t len = P->max_ntok;  // tokens of a segment
     if (!P->all_single && P->n_cu > 0 && P->n_seq * hkv < P->n_cu) {
-        const int64_t want = std::max<int64_t>(2 * P->n_cu / hkv, 1);  // segments
+        // Two workgroups a CU, half of that where a KV head's query heads can share
+        // one's work (launch_linear_chunk), of at least two tiles.  Each segment's
+        // state is written, scanned and read, 4 D^2 floats of traffic (32 heads of
+        // 8192 tokens, D = 128: 8 segments 156 us, 12 151, 16 137, 24 159; 4 heads of
+        // G = 8, in two parts: 16 segments 94 us, 32 77, 64 78).
+        const int64_t want = std::max<int64_t>((P->lin.n_q_heads > hkv ? 1 : 2) * P->n_cu / hkv, 1);
         len = std::max<int64_t>(ceil_div(ceil_div(P->T, want), kLinTile) * kLinTile, 2 * kLinTile);
         auto segments = [&] {
             int64_t m = 0;
@@ -2052,13 +2057,14 @@ mtn_status mtn_attend_linear(mtn_pool *P, int32_t layer, const void *q, const vo
         a.hkv = c.n_kv_heads;
         a.d = c.head_dim;
         a.n_items = (int32_t)(P->lin_items.size() / kLinItem);
+        a.parts = 1;
         hipStream_t s = (hipStream_t)stream;
         hipEvent_t e0;
         if ((st = timing_begin(P, s, &e0))) return st;
         if (P->all_single)
             HIP_TRY(P, launch_linear_decode(c.io_dtype, a, P->n_cu, s));
         else
-            HIP_TRY(P, launch_linear_chunk(c.io_dtype, a, P->lin_max, P->lin_split, s));
+            HIP_TRY(P, launch_linear_chunk(c.io_dtype, a, P->lin_max, P->lin_split, P->n_cu, s));
         if ((st = timing_end(P, 5, e0, s))) return st;
         P->lin_done[layer] = 1;
         return MTN_OK;

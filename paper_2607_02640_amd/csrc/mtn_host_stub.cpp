@@ -80,7 +80,7 @@ bool prefill_mfma_supported(int dtype, int d, int g) {
 }
 bool linear_supported(int dtype, int d, int g) { return (dtype == 0 || dtype == 1) && (d == 64 || d == 128) && group_ok(g); }
 hipError_t launch_linear_decode(int, const LinArgs &, int, hipStream_t) { return hipErrorNotSupported; }
-hipError_t launch_linear_chunk(int, const LinArgs &, int, bool, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_linear_chunk(int, LinArgs, int, bool, int, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_linear_poison(float *, int64_t, int32_t, const uint8_t *, hipStream_t) { return hipErrorNotSupported; }
 
 }  // namespace mtn

@@ -24,13 +24,14 @@ struct LinArgs {
     const float *log2_decay;  // device [Hkv]
     float scale;
     int32_t hq, hkv, d, n_items;
+    int32_t parts;            // chunk form: workgroups that share a KV head's query heads
 };
 
 bool linear_supported(int dtype, int d, int g);
 // Plans of one token per sequence
 hipError_t launch_linear_decode(int dtype, const LinArgs &a, int n_cu, hipStream_t s);
 // Plans of any lengths; max_tok: the longest item, split: some sequence has segments
-hipError_t launch_linear_chunk(int dtype, const LinArgs &a, int max_tok, bool split, hipStream_t s);
+hipError_t launch_linear_chunk(int dtype, LinArgs a, int max_tok, bool split, int n_cu, hipStream_t s);
 // Debug: NaN into every state slot with dead[slot] != 0 (slots of slot_stride floats)
 hipError_t launch_linear_poison(float *states, int64_t slot_stride, int32_t n_slots, const uint8_t *dead,
                                 hipStream_t s);

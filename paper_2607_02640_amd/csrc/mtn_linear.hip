@@ -16,8 +16,13 @@
 namespace mtn {
 namespace {
 
-constexpr int kLinWaves = 4;
-constexpr int kLinThreads = 64 * kLinWaves;
+constexpr int kLinThreads = 256;  // of the single-token form
+// Waves of a chunk workgroup with tiles of B tokens.  Four with 64-token tiles: at
+// eight, a wave's operands served half as many products, and its registers (128 for
+// two workgroups a CU) spilled in the loop (one prompt of 8192 tokens of 32 heads
+// 144 us, 137 with four).  With 32-token tiles eight at D = 128 end sooner where
+// few workgroups run (32 sessions of 25 tokens, G = 4, 4 KV heads 16.5 us, four 18.0).
+constexpr int lin_waves(int d, int b) { return b == 64 ? 4 : d / 16; }
 
 // ---------------------------------------------------------------------------
 // recurrent form: one token per sequence
@@ -122,19 +127,19 @@ struct Ops<bf16_t> {
     // scores (2^-15).
     static constexpr int kOut = 2, kState = 3;
     static __device__ __forceinline__ Frag row(const bf16_t *p) { return *(const uint4 *)p; }
-    // rows (tokens) of p0 and p1, a column a lane: see tr()
-    static __device__ __forceinline__ uint2 tr(const bf16_t *p) {
-        typedef __attribute__((ext_vector_type(4))) short s16x4;
-        return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                             (__attribute__((address_space(3))) s16x4 *)(
-                                                 const __attribute__((address_space(3))) void *)p));
+    typedef __attribute__((ext_vector_type(4))) short s16x4;
+    static __device__ __forceinline__ s16x4 tr(const bf16_t *p) {
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4 *)(const __attribute__((address_space(3))) void *)p);
     }
     // Four tokens of two tiles for column n: lane (n, g) hands in the address of
     // columns 4 (n % 4) .. + 3 (wherever those lie) of token 4 g + n / 4 and
     // receives column n of tokens 4 g .. + 3.
-    static __device__ __forceinline__ Frag cols(const bf16_t *p, int tile_stride, int, int) {
-        const uint2 x = tr(p), y = tr(p + tile_stride);
-        return make_uint4(x.x, x.y, y.x, y.y);
+    // p(row, column): where an element of the token array lies
+    template <class P>
+    static __device__ __forceinline__ Frag cols(P &&p, int t0, int g, int n, int col4, int) {
+        const s16x4 x = tr(p(t0 + 4 * g + (n >> 2), col4)), y = tr(p(t0 + 16 + 4 * g + (n >> 2), col4));
+        return __builtin_bit_cast(uint4, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     }
     static __device__ __forceinline__ f32x4_t mma(const Frag &a, const Frag &b, f32x4_t c) {
         return mfma16x16x32(a, b, c);
@@ -160,14 +165,16 @@ struct Ops<bf16_t> {
             f[p] = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
-    // largest magnitude's bits reach the exponent of infinities
-    static __device__ __forceinline__ bool bad(const Frag &f) {
-        const uint32_t w[4] = {f.x, f.y, f.z, f.w};
-        bool b = false;
+    // is some element not finite?
+    template <int N>
+    static __device__ __forceinline__ bool bad(const Frag (&f)[N]) {
+        typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+        u16x2 m = {0, 0};
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            b |= (w[e] & 0x7F80u) == 0x7F80u || (w[e] & 0x7F800000u) == 0x7F800000u;
-        return b;
+        for (int i = 0; i < N; ++i)
+            for (const uint32_t w : {f[i].x, f[i].y, f[i].z, f[i].w})
+                m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu));
+        return m[0] >= 0x7F80 || m[1] >= 0x7F80;
     }
     static __device__ __forceinline__ bool bad_at(const Frag &f, int e) {
         const uint32_t w[4] = {f.x, f.y, f.z, f.w};
@@ -198,14 +205,14 @@ struct Ops<float> {
         *(float4 *)&f.x[4] = *(const float4 *)(p + 4);
         return f;
     }
-    // the lane's own column (n % 4 of those handed in), token by token
-    static __device__ __forceinline__ Frag cols(const float *p, int tile_stride, int ld, int n) {
+    // the lane's own column, token by token
+    template <class P>
+    static __device__ __forceinline__ Frag cols(P &&p, int t0, int g, int, int, int col) {
         Frag f;
-        const float *c = p - (n >> 2) * ld;  // token 4 g
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            f.x[e] = c[e * ld];
-            f.x[4 + e] = c[tile_stride + e * ld];
+            f.x[e] = *p(t0 + 4 * g + e, col);
+            f.x[4 + e] = *p(t0 + 16 + 4 * g + e, col);
         }
         return f;
     }
@@ -224,10 +231,13 @@ struct Ops<float> {
         for (int e = 0; e < 8; ++e) f[0].x[e] = x[e];
     }
     static __device__ __forceinline__ bool bad_at(const Frag &f, int e) { return !(fabsf(f.x[e]) < INFINITY); }
-    static __device__ __forceinline__ bool bad(const Frag &f) {
+    template <int N>
+    static __device__ __forceinline__ bool bad(const Frag (&f)[N]) {
         bool b = false;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) b |= bad_at(f, e);
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) b |= bad_at(f[i], e);
         return b;
     }
     static __device__ __forceinline__ void clear_at(Frag &f, int e) { f.x[e] = 0.f; }
@@ -238,14 +248,20 @@ struct Ops<float> {
     }
 };
 
+// (a vector times a scalar keeps four copies of the scalar)
+__device__ __forceinline__ void scale4(f32x4_t &x, float f) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] *= f;
+}
+
 // ---------------------------------------------------------------------------
 // chunk form
 // ---------------------------------------------------------------------------
-// One workgroup of four waves per (item, KV head), tiles of B tokens one after the
+// One workgroup per (item, KV head), tiles of B tokens one after the
 // other.  With S before the tile, i and j tokens of the tile, n its length:
 //   o_i  = scale (lambda^(i+1) S q_i + sum_{j <= i} lambda^(i-j) (k_j . q_i) v_j)
 //   S'   = lambda^n S + sum_j (lambda^(n-1-j) v_j) k_j^T
-// A wave owns D / 4 value dims: their rows of S stay in its accumulators from the
+// A wave owns 16 or 32 value dims: their rows of S stay in its accumulators from the
 // first tile to the last, and serve as an operand of S q as they lie (two
 // accumulators make a fragment's depth).  Scores are formed transposed (keys by
 // queries), each wave those of one 16-query tile, and go through LDS to
@@ -262,68 +278,75 @@ struct Ops<float> {
 // and 0 * inf is NaN, so a wave whose values hold one clears it, and writes
 // NaN into that dim's outputs from that token on.
 template <typename T, int D, int B, bool LOCAL>
-__global__ __launch_bounds__(kLinThreads, 1) void k_linear_chunk(LinArgs a) {
+__global__ __launch_bounds__(64 * lin_waves(D, B), lin_waves(D, B) / 2) void k_linear_chunk(LinArgs a) {
     using O = Ops<T>;
     using Frag = typename O::Frag;
-    constexpr int NT = D / 64, NS = D / 32, MT = D / 16, JT = B / 16, KS = B / 32;
-    constexpr int EPV = 16 / (int)sizeof(T), LD = D + EPV;  // row pitch in LDS
-    constexpr int VPR = D / EPV;                            // vectors of a row
-    constexpr int CH = B * VPR / kLinThreads;
-    static_assert(B * VPR % kLinThreads == 0 && JT <= kLinWaves, "tile shape");
-    __shared__ __align__(16) T sk[B * LD], sv[B * LD], sq[LOCAL ? EPV : B * LD];
+    constexpr int NW = lin_waves(D, B), kThreads = 64 * NW;
+    constexpr int NT = D / (16 * NW), NS = D / 32, MT = D / 16, JT = B / 16, KS = B / 32;
+    constexpr int KW = NW >= 2 * JT ? 1 : KS;  // 32-key slices of scores per wave
+    constexpr int kMG = sizeof(T) == 2 ? 4 : 2;  // tiles of S updated side by side
+    constexpr int EPV = 16 / (int)sizeof(T);  // elements of a vector
+    constexpr int VPR = D / EPV;              // vectors of a row
+    constexpr int LD = sizeof(T) == 2 ? D : D + EPV;  // pitch of a row in LDS
+    constexpr int CH = B * VPR / kThreads;
+    static_assert(B * VPR % kThreads == 0 && JT <= NW && (NT == 1 || NT == 2), "tile shape");
+    __shared__ __align__(256) T sk[B * LD], sv[B * LD], sq[LOCAL ? EPV : B * LD];
     __shared__ Frag sp[LOCAL ? 1 : JT * KS * O::kOut * 64];
+    __shared__ __align__(16) float pw[B + 1], pr[B];  // lambda^m; lambda^(B - 1 - m)
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, n = lane & 15, g = lane >> 4;
-    const int it_ = (int)(blockIdx.x / (uint32_t)a.hkv), h = (int)(blockIdx.x - (uint32_t)it_ * a.hkv);
+    // (item, KV head, part of its query heads)
+    const uint32_t unit = LOCAL ? blockIdx.x : blockIdx.x / (uint32_t)a.parts;
+    const int part = LOCAL ? 0 : (int)(blockIdx.x - unit * (uint32_t)a.parts);
+    const int it_ = (int)(unit / (uint32_t)a.hkv), h = (int)(unit - (uint32_t)it_ * a.hkv);
     const int row0 = scalar_ld(a.items, kLinItem * it_), ntok = scalar_ld(a.items, kLinItem * it_ + 1);
     const int rec = scalar_ld(a.items, kLinItem * it_ + 2);
     const int nseg = scalar_ld(a.items, kLinItem * it_ + 3) >> 16;
     if (LOCAL && nseg == 1) return;  // the whole workgroup
-    const int slot = rec & (kLinFresh - 1), G = a.hq / a.hkv;
+    const int slot = rec & (kLinFresh - 1);
+    const int G = a.hq / a.hkv / a.parts, hq0 = (h * a.parts + part) * G;  // this workgroup's query heads
     const float l2 = a.log2_decay[h];
-    auto power = [&](int e) { return __builtin_amdgcn_exp2f((float)e * l2); };
-
+    for (int m = tid; m <= B; m += kThreads) {
+        const float x = __builtin_amdgcn_exp2f((float)m * l2);
+        pw[m] = x;
+        if (m < B) pr[B - 1 - m] = x;
+    }
+    // Token rows in LDS, laid so that sixteen rows' vectors of one column, a
+    // fragment's, lie in different banks: bf16 vector x of a row at x ^ its swizzle,
+    // fp32 rows a vector apart (their single elements are read by column, too).
+    auto at = [](T *base, int row, int col) {
+        const int sw = sizeof(T) == 4 ? 0 : VPR == 16 ? row & 15 : (row >> 1) & 7;
+        return base + row * LD + ((col / EPV) ^ sw) * EPV + col % EPV;
+    };
     // this wave's value dims: lane n of tile nt is dim dv0 + dvn + 4 nt, result row
     // 4 g + r dim dv0 + 8 g + 4 nt + r (one tile: n and 4 g + r)
     const int dv0 = wv * 16 * NT;
     const int dvn = NT == 2 ? 8 * (n >> 2) + (n & 3) : n;
-    // S as the products make it: result row 4 g + r of tile mt = 2 s + t is key dim
-    // 32 s + 8 g + 4 t + r, column n the value dim above
-    f32x4_t S[MT][NT];
-    float *const seg = a.seg + ((int64_t)it_ * a.hkv + h) * D * D;
-    {
-        const float *src = nseg > 1 ? seg : a.state + (int64_t)slot * a.slot_stride + (int64_t)h * D * D;
-        const bool zero = LOCAL || (nseg == 1 && (rec & kLinFresh));
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-                S[m][nt] = zero ? f32x4_t{0.f, 0.f, 0.f, 0.f}
-                                : *(const f32x4_t *)(src + (dv0 + dvn + 4 * nt) * D + 32 * (m / 2) + 8 * g + 4 * (m & 1));
-    }
-    // decays of this wave's scores (queries 16 wv + n) and of the outputs' rows
-    float wp[JT][4], wr[JT];
-    if constexpr (!LOCAL) {
-#pragma unroll
-        for (int jt = 0; jt < JT; ++jt) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) wp[jt][r] = power(max(16 * (wv - jt) + n - 4 * g - r, 0));
-            wr[jt] = power(16 * jt + n + 1);
-        }
-    }
-    // 16 bytes of token row, vector col of a tile, per thread and step
+    // this wave's scores: queries of tile wv % JT, key slices wv / JT + kk
+    const int pit = wv % JT, pks = wv / JT;
+    const int pd = 16 * pit + n - 32 * pks - 4 * g;  // query - key of the lane's first score
+    auto key = [](int e) { return 16 * (e / 4) + (e & 3); };  // ... and its others, from there
+    // A thread's vectors of the nb tokens from t0 (the last token's in place of those
+    // behind it), and into LDS (zeros behind the last token).
     auto load = [&](const void *base, int heads, int head, int t0, int nb, uint4 (&x)[CH]) __attribute__((always_inline)) {
         const T *p = (const T *)base + ((int64_t)(row0 + t0) * heads + head) * D;
+        uint32_t t = tid;
+        asm volatile("" : "+v"(t));  // (what it makes is not kept over the loop, in registers)
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int v = tid + c * kLinThreads, r = v / VPR;
-            x[c] = r < nb ? *(const uint4 *)(p + (int64_t)r * heads * D + v % VPR * EPV) : make_uint4(0, 0, 0, 0);
+            const uint32_t v = t + c * kThreads;
+            x[c] = *(const uint4 *)(p + (min(v / VPR, (uint32_t)nb - 1) * (uint32_t)(heads * D) + v % VPR * EPV));
         }
     };
-    auto put = [&](T *dst, const uint4 (&x)[CH]) __attribute__((always_inline)) {
+    auto put = [&](T *dst, uint4 (&x)[CH], int nb) __attribute__((always_inline)) {
+        if (nb < B) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+                if ((tid + c * kThreads) / VPR >= nb) x[c] = make_uint4(0, 0, 0, 0);
+        }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int v = tid + c * kLinThreads;
-            *(uint4 *)(dst + v / VPR * LD + v % VPR * EPV) = x[c];
+            const int v = tid + c * kThreads;
+            *(uint4 *)at(dst, v / VPR, v % VPR * EPV) = x[c];
         }
     };
     uint4 xk[CH], xv[CH], xq[CH];
@@ -331,72 +354,115 @@ __global__ __launch_bounds__(kLinThreads, 1) void k_linear_chunk(LinArgs a) {
         const int nb = min(B, ntok);
         load(a.k, a.hkv, h, 0, nb, xk);
         load(a.v, a.hkv, h, 0, nb, xv);
-        if constexpr (!LOCAL) load(a.q, a.hq, h * G, 0, nb, xq);
+        if constexpr (!LOCAL) load(a.q, a.hq, hq0, 0, nb, xq);
+    }
+    // (behind the rows, which are needed first)
+    // S as the products make it: result row 4 g + r of tile mt = 2 s + t is key dim
+    // 32 s + 8 g + 4 t + r, column n the value dim above
+    f32x4_t S[MT][NT];
+    float *const seg = a.seg + ((int64_t)it_ * a.hkv + h) * D * D;
+    {
+        const float *src = nseg > 1 ? seg : a.state + (int64_t)slot * a.slot_stride + (int64_t)h * D * D;
+        if (LOCAL || (nseg == 1 && (rec & kLinFresh))) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) S[m][nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        } else {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+                    S[m][nt] = *(const f32x4_t *)(src + (dv0 + dvn + 4 * nt) * D + 32 * (m / 2) + 8 * g + 4 * (m & 1));
+        }
     }
     for (int t0 = 0; t0 < ntok; t0 += B) {
         const int nb = min(B, ntok - t0);
-        put(sk, xk);
-        put(sv, xv);
-        if constexpr (!LOCAL) put(sq, xq);
+        put(sk, xk, nb);
+        put(sv, xv, nb);
+        if constexpr (!LOCAL) put(sq, xq, nb);
         __syncthreads();
-        auto next_tile = [&]() __attribute__((always_inline)) {
-            if (t0 + B >= ntok) return;
-            const int nx = min(B, ntok - t0 - B);
-            load(a.k, a.hkv, h, t0 + B, nx, xk);
-            load(a.v, a.hkv, h, t0 + B, nx, xv);
-            if constexpr (!LOCAL) load(a.q, a.hq, h * G, t0 + B, nx, xq);
-        };
         // values of this wave's dims, tokens deep
         Frag vf[KS][NT];
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-                vf[ks][nt] = O::cols(sv + (32 * ks + 4 * g + (n >> 2)) * LD + dv0 +
-                                         (NT == 2 ? 8 * (n & 3) + 4 * nt : 4 * (n & 3)) * (sizeof(T) == 2 ? 1 : 0) +
-                                         (sizeof(T) == 2 ? 0 : dvn + 4 * nt),
-                                     16 * LD, LD, n);
-        if constexpr (LOCAL) next_tile();
-        if constexpr (!LOCAL) {
-            bool bad = false;
+        auto values = [&]() __attribute__((always_inline)) {
+            int n1 = n, g1 = g;
+            asm volatile("" : "+v"(n1), "+v"(g1));  // (what they make is not kept over the loop, in registers)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) bad |= O::bad(vf[ks][nt]);
-            const bool any_bad = __builtin_amdgcn_ballot_w64(bad) != 0;
-            for (int gh = 0; gh < G; ++gh) {
-                if (gh + 1 < G)
-                    load(a.q, a.hq, h * G + gh + 1, t0, nb, xq);
-                else
-                    next_tile();
-                // ---- scores of queries 16 wv .. + 15, keys by queries
-                if (wv < JT && 16 * wv < nb) {
-                    f32x4_t sc[JT];
+                for (int nt = 0; nt < NT; ++nt)
+                    vf[ks][nt] = O::cols([&](int r, int c) { return at(sv, r, c); }, 32 * ks, g1, n1,
+                                         dv0 + (NT == 2 ? 8 * (n1 & 3) + 4 * nt : 4 * (n1 & 3)),
+                                         dv0 + 4 * nt + (NT == 2 ? 8 * (n1 >> 2) + (n1 & 3) : n1));
+        };
+        values();
+        bool any_bad = false;
+        // the next tile's keys and values, in flight through this one (nothing to keep
+        // where there is none)
+        uint4 yk[CH], yv[CH], yq[CH];
+        if (t0 + B < ntok) {
+            load(a.k, a.hkv, h, t0 + B, min(B, ntok - t0 - B), yk);
+            load(a.v, a.hkv, h, t0 + B, min(B, ntok - t0 - B), yv);
+        }
+        if constexpr (!LOCAL) {
+            // a value that is not finite: out of the products with scores, and into
+            // the outputs from its token on
+            bool bad = false;
+            int first[NT];
 #pragma unroll
-                    for (int jt = 0; jt < JT; ++jt) sc[jt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int nt = 0; nt < NT; ++nt) first[nt] = B;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) bad |= O::bad(vf[ks]);
+            any_bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+            if (__builtin_expect(any_bad, 0)) {
+                int g1 = g;
+                asm volatile("" : "+v"(g1));  // (as above)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (O::bad_at(vf[ks][nt], e)) {
+                                O::clear_at(vf[ks][nt], e);
+                                first[nt] = min(first[nt], 32 * ks + 4 * g1 + key(e));
+                            }
+                    first[nt] = min(first[nt], __shfl_xor(first[nt], 16, 64));
+                    first[nt] = min(first[nt], __shfl_xor(first[nt], 32, 64));
+                }
+            }
+            for (int gh = 0; gh < G; ++gh) {
+                {   // the next head's queries, or the next tile's (or, last, these once more)
+                    const bool more = gh + 1 < G;
+                    const int tq = !more && t0 + B < ntok ? t0 + B : t0;
+                    load(a.q, a.hq, hq0 + (more ? gh + 1 : 0), tq, min(B, ntok - tq), yq);
+                }
+                // ---- scores, keys by queries
+                int pdl = pd, n1 = n;
+                asm volatile("" : "+v"(pdl), "+v"(n1));  // (what they make is not kept over the loop, in registers)
+#pragma unroll
+                for (int kk = 0; kk < KW; ++kk) {
+                    const int ks = pks + kk;
+                    if (2 * ks > pit || 16 * pit >= nb) break;
+                    f32x4_t sc[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
                     for (int s = 0; s < NS; ++s) {
-                        const Frag qf = O::row(sq + (16 * wv + n) * LD + 32 * s + 8 * g);
+                        const Frag qf = O::row(at(sq, 16 * pit + n1, 32 * s + 8 * g));
 #pragma unroll
-                        for (int jt = 0; jt < JT; ++jt)
-                            if (jt <= wv) sc[jt] = O::mma(O::row(sk + (16 * jt + n) * LD + 32 * s + 8 * g), qf, sc[jt]);
+                        for (int j = 0; j < 2; ++j)
+                            sc[j] = O::mma(O::row(at(sk, 32 * ks + 16 * j + n1, 32 * s + 8 * g)), qf, sc[j]);
                     }
+                    float x[8];
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) {
-                        if (2 * ks > wv) break;
-                        float x[8];
+                    for (int e = 0; e < 8; ++e)
+                        x[e] = pdl >= 32 * kk + key(e) ? sc[e / 4][e & 3] * pw[max(pdl - 32 * kk - key(e), 0)] : 0.f;
+                    Frag pf[O::kOut];
+                    O::template split<O::kOut>(x, pf);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const int jt = 2 * ks + e / 4, r = e & 3;
-                            x[e] = 16 * jt + 4 * g + r <= 16 * wv + n ? sc[jt][r] * wp[jt][r] : 0.f;
-                        }
-                        Frag pf[O::kOut];
-                        O::template split<O::kOut>(x, pf);
-#pragma unroll
-                        for (int p = 0; p < O::kOut; ++p) sp[((wv * KS + ks) * O::kOut + p) * 64 + lane] = pf[p];
-                    }
+                    for (int p = 0; p < O::kOut; ++p) sp[((pit * KS + ks) * O::kOut + p) * 64 + lane] = pf[p];
                 }
                 // ---- S q, value dims by queries
+                asm volatile("" : "+v"(n1));
                 f32x4_t o[JT][NT];
 #pragma unroll
                 for (int it = 0; it < JT; ++it)
@@ -409,100 +475,98 @@ __global__ __launch_bounds__(kLinThreads, 1) void k_linear_chunk(LinArgs a) {
                     for (int nt = 0; nt < NT; ++nt) {
                         float x[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = S[2 * s + e / 4][nt][e & 3];
+                        for (int e = 0; e < 8; ++e) {
+                            // (split anew for every head: kept, the terms of all of S
+                            // would take as many registers as S)
+                            asm volatile("" : "+v"(S[2 * s + e / 4][nt][e & 3]));
+                            x[e] = S[2 * s + e / 4][nt][e & 3];
+                        }
                         O::template split<O::kOut>(x, sf[nt]);
                     }
+                    // (each term over all tiles: products in a row that do not wait for
+                    // one another)
+                    Frag qf[JT];
 #pragma unroll
-                    for (int it = 0; it < JT; ++it) {
-                        const Frag qf = O::row(sq + (16 * it + n) * LD + 32 * s + 8 * g);
+                    for (int it = 0; it < JT; ++it) qf[it] = O::row(at(sq, 16 * it + n1, 32 * s + 8 * g));
+#pragma unroll
+                    for (int p = 0; p < O::kOut; ++p)
+#pragma unroll
+                        for (int it = 0; it < JT; ++it)
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) o[it][nt] = O::mma(sf[nt][p], qf[it], o[it][nt]);
+                }
+                __syncthreads();  // every score is there, nobody reads these queries any more
+                if (gh + 1 < G) put(sq, yq, nb);
+                // ---- plus V times the scores
+                T *ob = (T *)a.out + ((int64_t)(row0 + t0) * a.hq + hq0 + gh) * D + dv0;
+                int i1 = n + 1;  // (as above)
+                asm volatile("" : "+v"(i1));
+                const uint32_t oo = (uint32_t)((i1 - 1) * a.hq * D + (NT == 2 ? 8 : 4) * g);
+#pragma unroll
+                for (int it = 0; it < JT; ++it)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) scale4(o[it][nt], pw[16 * it + i1]);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    if (32 * ks >= nb) break;
+#pragma unroll
+                    for (int p = 0; p < O::kOut; ++p) {
+                        Frag pf[JT];
+#pragma unroll
+                        for (int it = 2 * ks; it < JT; ++it) pf[it] = sp[((it * KS + ks) * O::kOut + p) * 64 + lane];
+#pragma unroll
+                        for (int it = 2 * ks; it < JT; ++it)
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) o[it][nt] = O::mma(vf[ks][nt], pf[it], o[it][nt]);
+                    }
+                }
+#pragma unroll
+                for (int it = 0; it < JT; ++it) {
+                    if (16 * it >= nb) break;
+                    const int i = 16 * it + i1 - 1;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) scale4(o[it][nt], a.scale);
+                    if (__builtin_expect(any_bad, 0)) {
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int p = 0; p < O::kOut; ++p) o[it][nt] = O::mma(sf[nt][p], qf, o[it][nt]);
+                            for (int r = 0; r < 4; ++r)
+                                if (i >= __shfl(first[nt], 4 * g + r, 64)) o[it][nt][r] = __builtin_nanf("");
+                    }
+                    if (i < nb) {
+                        T *p = ob + (int64_t)16 * it * a.hq * D + oo;
+                        if constexpr (NT == 2)
+                            O::store8(p, o[it][0], o[it][NT - 1]);
+                        else
+                            O::store4(p, o[it][0]);
                     }
                 }
-                __syncthreads();  // every score is there, nobody reads these queries any more
-                if (gh + 1 < G) put(sq, xq);
-                // ---- plus V times the scores
-                T *ob = (T *)a.out + ((int64_t)(row0 + t0) * a.hq + h * G + gh) * D + dv0;
-                auto finish = [&](auto bad_c) __attribute__((always_inline)) {
-                    constexpr bool BAD = decltype(bad_c)::value;
-                    int first[NT];  // BAD: the first token whose value of the lane's dim is not finite
-                    Frag vc[BAD ? KS : 1][NT];
-                    if constexpr (BAD) {
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            first[nt] = B;
-#pragma unroll
-                            for (int ks = 0; ks < KS; ++ks) {
-                                vc[ks][nt] = vf[ks][nt];
-#pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    if (O::bad_at(vf[ks][nt], e)) {
-                                        O::clear_at(vc[ks][nt], e);
-                                        first[nt] = min(first[nt], 32 * ks + 16 * (e / 4) + 4 * g + (e & 3));
-                                    }
-                            }
-                            first[nt] = min(first[nt], __shfl_xor(first[nt], 16, 64));
-                            first[nt] = min(first[nt], __shfl_xor(first[nt], 32, 64));
-                        }
-                    }
-#pragma unroll
-                    for (int it = 0; it < JT; ++it) {
-                        if (16 * it >= nb) break;
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) o[it][nt] *= wr[it];
-#pragma unroll
-                        for (int ks = 0; ks < KS; ++ks) {
-                            if (2 * ks > it) break;
-#pragma unroll
-                            for (int p = 0; p < O::kOut; ++p) {
-                                const Frag pf = sp[((it * KS + ks) * O::kOut + p) * 64 + lane];
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt)
-                                    o[it][nt] = O::mma(BAD ? vc[BAD ? ks : 0][nt] : vf[ks][nt], pf, o[it][nt]);
-                            }
-                        }
-                        const int i = 16 * it + n;
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            o[it][nt] *= a.scale;
-                            if constexpr (BAD) {
-#pragma unroll
-                                for (int r = 0; r < 4; ++r)
-                                    if (i >= __shfl(first[nt], 4 * g + r, 64)) o[it][nt][r] = __builtin_nanf("");
-                            }
-                        }
-                        if (i < nb) {
-                            T *p = ob + (int64_t)i * a.hq * D;
-                            if constexpr (NT == 2)
-                                O::store8(p + 8 * g, o[it][0], o[it][NT - 1]);
-                            else
-                                O::store4(p + 4 * g, o[it][0]);
-                        }
-                    }
-                };
-                if (__builtin_expect(any_bad, 0))
-                    finish(std::true_type{});
-                else
-                    finish(std::false_type{});
                 if (gh + 1 < G) __syncthreads();  // the next queries are there, the scores read
             }
         }
         // ---- the state after the tile
-        if (LOCAL || nseg == 1 || t0 + B < ntok) {
-            const float dec = power(nb);
+        if (LOCAL || (nseg == 1 && part == 0) || t0 + B < ntok) {
+            if (__builtin_expect(any_bad, 0)) values();  // as they are
+            const float dec = pw[nb];
+            int left = nb - 1 - 4 * g;  // tokens after the lane's first
+            int n1 = n, g1 = g;
+            asm volatile("" : "+v"(left), "+v"(n1), "+v"(g1));  // (as above)
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) S[m][nt] *= dec;
+                for (int nt = 0; nt < NT; ++nt) scale4(S[m][nt], dec);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 if (32 * ks >= nb) break;
                 Frag vw[NT][O::kState];
                 float w[8];
+                if (nb == B) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = power(max(nb - 1 - (32 * ks + 16 * (e / 4) + 4 * g + (e & 3)), 0));
+                    for (int u = 0; u < 2; ++u) *(f32x4_t *)&w[4 * u] = *(const f32x4_t *)&pr[32 * ks + 16 * u + 4 * g];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = pw[max(left - 32 * ks - key(e), 0)];
+                }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     float x[8];
@@ -512,20 +576,33 @@ __global__ __launch_bounds__(kLinThreads, 1) void k_linear_chunk(LinArgs a) {
                     O::template split<O::kState>(x, vw[nt]);
                 }
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const Frag kf = O::cols(sk + (32 * ks + 4 * g + (n >> 2)) * LD + 32 * (m / 2) + 4 * (m & 1) +
-                                                (sizeof(T) == 2 ? 8 * (n & 3) : 8 * (n >> 2) + (n & 3)),
-                                            16 * LD, LD, n);
+                for (int m0 = 0; m0 < MT; m0 += kMG) {
+                    Frag kf[kMG];
+#pragma unroll
+                    for (int j = 0; j < kMG; ++j) {
+                        const int c = 32 * ((m0 + j) / 2) + 4 * (j & 1);
+                        kf[j] = O::cols([&](int r, int c) { return at(sk, r, c); }, 32 * ks, g1, n1, c + 8 * (n1 & 3),
+                                        c + 8 * (n1 >> 2) + (n1 & 3));
+                    }
 #pragma unroll
                     for (int p = 0; p < O::kState; ++p)
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) S[m][nt] = O::mma(kf, vw[nt][p], S[m][nt]);
+                        for (int j = 0; j < kMG; ++j)
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+                                S[m0 + j][nt] = O::mma(kf[j], vw[nt][p], S[m0 + j][nt]);
                 }
             }
         }
         __syncthreads();  // K, V, Q and scores may be overwritten
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            xk[c] = yk[c];
+            xv[c] = yv[c];
+            if constexpr (!LOCAL) xq[c] = yq[c];
+        }
     }
-    if (!LOCAL && nseg > 1) return;
+    if (!LOCAL && (nseg > 1 || part)) return;
     float *dst = LOCAL ? seg : a.state + (int64_t)(slot ^ 1) * a.slot_stride + (int64_t)h * D * D;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -602,13 +679,25 @@ bool linear_supported(int dtype, int d, int g) {
 hipError_t launch_linear_decode(int dtype, const LinArgs &a, int n_cu, hipStream_t s) {
     if (!linear_supported(dtype, a.d, a.hq / a.hkv) || a.n_items < 1) return hipErrorInvalidValue;
     const int64_t units = (int64_t)a.n_items * a.hkv;
-    if (2 * units > INT32_MAX) return hipErrorInvalidValue;
+    if (4 * units > INT32_MAX) return hipErrorInvalidValue;
     return by_shape(dtype, a.d, [&](auto dc, auto elt) {
         constexpr int D = decltype(dc)::value;
         using T = decltype(elt);
         auto go = [&](auto gc) {
-            hipLaunchKernelGGL((k_linear_decode<T, D, decltype(gc)::value, 1>), dim3((unsigned)units),
-                               dim3(kLinThreads), 0, s, a);
+            constexpr int G = decltype(gc)::value, kMost = D / 32;
+            auto sliced = [&](auto sc) {
+                constexpr int SL = decltype(sc)::value;
+                hipLaunchKernelGGL((k_linear_decode<T, D, G, SL>), dim3((unsigned)(units * SL)), dim3(kLinThreads), 0,
+                                   s, a);
+            };
+            // rows of a state over several workgroups where states are few (32 sessions,
+            // G = 4, 4 heads 9.7 us whole, 8.0 in four slices; 512 states of G = 8 19.2
+            // whole, 21.0 in two)
+            int sl = 1;
+            while (sl < kMost && 2 * sl * units <= 2 * (int64_t)n_cu) sl *= 2;
+            if (sl == 1) return sliced(std::integral_constant<int, 1>{});
+            if (sl == 2 || kMost == 2) return sliced(std::integral_constant<int, 2>{});
+            sliced(std::integral_constant<int, kMost>{});
         };
         switch (a.hq / a.hkv) {
             case 1: go(std::integral_constant<int, 1>{}); break;
@@ -619,24 +708,34 @@ hipError_t launch_linear_decode(int dtype, const LinArgs &a, int n_cu, hipStream
     });
 }
 
-hipError_t launch_linear_chunk(int dtype, const LinArgs &a, int max_tok, bool split, hipStream_t s) {
+hipError_t launch_linear_chunk(int dtype, LinArgs a, int max_tok, bool split, int n_cu, hipStream_t s) {
     if (!linear_supported(dtype, a.d, a.hq / a.hkv) || a.n_items < 1 || (split && !a.seg)) return hipErrorInvalidValue;
     const int64_t units = (int64_t)a.n_items * a.hkv;
     if (units > (split ? 65535 : INT32_MAX)) return hipErrorInvalidValue;  // (the scan's second grid dimension)
+    // 32-token tiles take chunks up to 32 tokens and fp32; the query heads of a KV head
+    // go to several workgroups, each with the state, where that fills the CUs: with a
+    // workgroup of eight waves each, or two of four (one session of 25 tokens, G = 4,
+    // 4 KV heads 14.9 us whole, 10.5 in four parts; 32 sessions 16.6, 15.3 in two, 18.5
+    // in four; 8192 tokens of G = 8, 4 KV heads, 64 segments 90.3 whole, 77.7 in two,
+    // 89.3 in four).
+    const int tile = dtype == 1 && max_tok > 32 ? 64 : 32;
+    a.parts = 1;
+    while (2 * a.parts * units <= (tile == 64 ? 2 : 1) * (int64_t)n_cu && a.hq / a.hkv % (2 * a.parts) == 0) a.parts *= 2;
     return by_shape(dtype, a.d, [&](auto dc, auto elt) {
         constexpr int D = decltype(dc)::value;
         using T = decltype(elt);
         auto go = [&](auto bc) {
             constexpr int B = decltype(bc)::value;
-            const dim3 grid((unsigned)units), block(kLinThreads);
+            const dim3 grid((unsigned)units), block(64 * lin_waves(D, B));
+            const dim3 grid2((unsigned)(units * a.parts));
             if (split) {
                 hipLaunchKernelGGL((k_linear_chunk<T, D, B, true>), grid, block, 0, s, a);
                 hipLaunchKernelGGL((k_linear_scan<D>), dim3(D * D / 1024, (unsigned)units), dim3(256), 0, s, a);
             }
-            hipLaunchKernelGGL((k_linear_chunk<T, D, B, false>), grid, block, 0, s, a);
+            hipLaunchKernelGGL((k_linear_chunk<T, D, B, false>), grid2, block, 0, s, a);
         };
         if constexpr (sizeof(T) == 2) {
-            if (max_tok > 32) return go(std::integral_constant<int, 64>{});
+            if (tile == 64) return go(std::integral_constant<int, 64>{});
         }
         go(std::integral_constant<int, 32>{});
     });
