@@ -231,6 +231,10 @@ def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream
     import torch
+    if torch.cuda.is_initialized():
+        # what current_stream().cuda_stream returns, without the Stream object, which
+        # took half of a call's time on the host (3.4 of 6.6 us)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if torch.cuda.is_available():
         return torch.cuda.current_stream().cuda_stream
     return None
