@@ -22,6 +22,7 @@ struct LinArgs {
     int64_t slot_stride;      // floats from a slot to the next
     float *seg;               // segments' states [item][Hkv][D][D]
     const float *log2_decay;  // device [Hkv]
+    const float *decay[2];    // device [Hkv]: e^log_decay in two terms
     float scale;
     int32_t hq, hkv, d, n_items;
     int32_t parts;            // chunk form: workgroups that share a KV head's query heads

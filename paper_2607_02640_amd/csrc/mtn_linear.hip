@@ -31,8 +31,11 @@ constexpr int lin_waves(int d, int b) { return b == 64 ? 4 : d / 16; }
 // e holds S[e][0 .. D - 1].  Eight lanes share a row (16-byte vectors side by side,
 // whole 128-byte lines per load instruction), 32 rows per step of the workgroup;
 // every load of a thread's part of the state goes out before the first is used.
-// Each element takes one product and one multiply-add for its update and one
+// Each element takes one product and two multiply-adds for its update and one
 // more per query head: bound by the state's bytes, read and written once.
+// The decay comes in two fp32 terms: one that is rounded is off the same way token
+// after token (lambda = 1 - 2^-14 and a steady input: 2^-25 of lambda are 2^-11 of the
+// state it comes to), which roundings of the state are not.
 template <typename T, int D, int G, int SL>
 __global__ __launch_bounds__(kLinThreads) void k_linear_decode(LinArgs a) {
     constexpr int RW = D / SL;         // rows of the workgroup
@@ -65,7 +68,7 @@ __global__ __launch_bounds__(kLinThreads) void k_linear_decode(LinArgs a) {
     const T *kr = (const T *)a.k + (row * a.hkv + h) * D;
     for (int x = tid; x < G * D; x += kLinThreads) (&sq[0][0])[x] = to_f32(qr[x]);
     if (tid < D) sk[tid] = to_f32(kr[tid]);
-    const float lam = __builtin_amdgcn_exp2f(a.log2_decay[h]);
+    const float lam = a.decay[0][h], lam1 = a.decay[1][h];
     __syncthreads();
     float acc[NP][G];
 #pragma unroll
@@ -78,7 +81,7 @@ __global__ __launch_bounds__(kLinThreads) void k_linear_decode(LinArgs a) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) S[p][c][e] = fmaf(lam, S[p][c][e], v[p] * kk[e]);
+            for (int e = 0; e < 4; ++e) S[p][c][e] = fmaf(lam, S[p][c][e], fmaf(lam1, S[p][c][e], v[p] * kk[e]));
             *(f32x4_t *)(dst + (e0 + 32 * p) * D + c0 + 32 * c) = S[p][c];
         }
 #pragma unroll

@@ -287,3 +287,34 @@ def test_taken_away_and_given_again():
     y.sids, y.orc = [y.pool.session_open()], {0: y.fresh()}
     y.step([9])
     y.step([1])
+
+
+@pytest.mark.parametrize("a", [-2.0 ** -14, -3e-5, -0.0123, -0.7])
+def test_single_tokens_decay_without_drift(a):
+    """A state that nothing is added to is e^(n a) of what it was.  Each of n steps
+    rounds each of M elements on its own, by at most 2^-24 of it and at most twice (a
+    standard deviation of 2^-24 sqrt(2 / 3) at most): the mean of the M relative errors
+    is off by 2^-24 sqrt(2 n / (3 M)) (one deviation; six are allowed) and by what the
+    decay is off, n times over: 2^-48 for two terms of 24 bits."""
+    n, d = 600, 64
+    x = Linear("f32", 1, 1, d, log_decay=[[a]])
+    q, k, v = x.rows(1)
+    x.step([1], rows=(q, torch.randn_like(k), v))
+    state = x.pool.session_state(x.sids[0])
+    state.copy_(torch.rand_like(state) + 0.5)
+    before = f64(state)
+    zero = [torch.zeros_like(r) for r in (q, k, v)]
+    for _ in range(n):
+        x.plan(x.sids, [1])
+        x.attend(*zero)
+        x.pool.plan_commit()
+    got, ref = f64(x.pool.session_state(x.sids[0])), before * np.exp(n * float(np.float32(a)))
+    if ref.max() < 2.0 ** -126:
+        # relative errors end where fp32's normal numbers do (e^-420 is no fp32 number
+        # at all); what falls below them only falls further
+        assert got.min() >= 0.0 and got.max() < 2.0 ** -126
+        return
+    rel = got / ref - 1.0
+    say(f"a {a}: mean relative error {rel.mean():.2e}")
+    assert abs(rel.mean()) <= 6 * 2.0 ** -24 * np.sqrt(2 * n / (3 * d * d)) + n * 2.0 ** -48
+    assert np.abs(rel).max() <= 2 * n * 2.0 ** -24
