@@ -48,6 +48,10 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
     bf16x2_t v = {(__bf16)lo, (__bf16)hi};
     return __builtin_bit_cast(uint32_t, v);
 }
+// ... of what the packed pair p of them leaves
+__device__ __forceinline__ uint32_t bf16x2_rest(float lo, float hi, uint32_t p) {
+    return pack_bf16x2(lo - __uint_as_float(p << 16), hi - __uint_as_float(p & 0xFFFF0000u));
+}
 __device__ __forceinline__ float dot2_bf16(uint32_t a, uint32_t b, float c) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, a),
                                            __builtin_bit_cast(bf16x2_t, b), c, false);
@@ -143,7 +147,8 @@ __device__ __forceinline__ void wave_sync() {
 // and the probabilities are bf16 operands of the matrix instructions (outputs of
 // N(0, 1) rows are 0.0029 off in rms against 0.0018 with fp32 operands, which is the
 // output's own rounding; a second product for the query's low bits would be half as
-// many MFMAs again).
+// many MFMAs again).  The third takes operands in two terms where k_attn_mfma has idle
+// columns for them, and the chunk prefill's probabilities over fp8 blocks.
 inline int rope_form(const PoolGeom &g) {
     return g.rope_il & kRopeNorm ? 2 : g.rope_il || g.rope_half != g.d / 2;
 }

@@ -192,6 +192,18 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
 
     // ---- q prologue: rotate at pos, fold the softmax scale (log2 domain);
     // the B operand of QK MFMA s holds dims D/4 g4 + 8 s .. + 7 of head n.
+    // Normed: column n + 8, which no head has, takes what the rounding of head n's
+    // query and probabilities to bf16 leaves, as a second term, and the two columns'
+    // scores and sums are added, without another matrix instruction.  Outputs of
+    // N(0, 1) rows are off by their own rounding and that of the stored rows alone
+    // (rms 0.0025 over bf16 blocks, 0.0017 over fp8; with one term 0.0034 and 0.0029).
+    // 128 bf16 sessions over 2052 keys 89.1 us a launch, 88.5 with one term; 32 fp8
+    // sessions 20.7, 19.6 (22.0 with a branch for the second term, behind which the
+    // loads of one slice of the query waited for those of the slice before it).
+    constexpr bool kTwo = RF == 2;
+    static_assert(!kTwo || G <= 8, "columns for second terms");
+    const bool rest = kTwo && n >= 8;
+    const int hn = kTwo ? n & 7 : n;
     const int d0 = D / 4 * g4;
     uint4 qb[ND];
     NormView nw{};
@@ -199,8 +211,8 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
     const float2 *rp = a.p.rope + (int64_t)t * (D / 2) + (d0 & (D / 2 - 1));
     const float sgn = g4 < 2 ? -1.f : 1.f;
     {
-        const bool hv = n < G;
-        const bf16_t *qh = (const bf16_t *)a.q + (row * g.hq + (int64_t)kvh * G + (hv ? n : 0)) * D;
+        const bool hv = hn < G;
+        const bf16_t *qh = (const bf16_t *)a.q + (row * g.hq + (int64_t)kvh * G + (hv ? hn : 0)) * D;
         const bf16_t *qd = qh + d0, *qp = qh + (d0 ^ (D / 2));  // the dims and their partners
         auto load_pair = [&](int s, float (&x)[8], float (&y)[8]) __attribute__((always_inline)) {
             if constexpr (RF) {
@@ -244,7 +256,10 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
                 const float2 c0 = rp[8 * s + e], c1 = rp[8 * s + e + 1];
                 const float r0 = fmaf(x[e], c0.x, sgn * y[e] * c0.y) * a.scale_log2;
                 const float r1 = fmaf(x[e + 1], c1.x, sgn * y[e + 1] * c1.y) * a.scale_log2;
-                w[e / 2] = hv ? pack_bf16x2(r0, r1) : 0u;
+                uint32_t x = pack_bf16x2(r0, r1);
+                // (less nothing in the other columns: no branch, the loads stay ahead)
+                if constexpr (kTwo) x = bf16x2_rest(r0, r1, rest ? x : 0u);
+                w[e / 2] = hv ? x : 0u;
             }
             qb[s] = make_uint4(w[0], w[1], w[2], w[3]);
         }
@@ -405,6 +420,9 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
             }
             vw[0] = w0.x; vw[1] = w0.y; vw[2] = w0.z; vw[3] = w0.w;
             vw[4] = w1.x; vw[5] = w1.y; vw[6] = w1.z; vw[7] = w1.w;
+            if constexpr (kTwo)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) c[r] += dpp<kRowRor8>(c[r]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) sc[r] = c[r] * f8_scale(eks, r);
         } else {
@@ -415,7 +433,7 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
             for (int j = 0; j < NJ; ++j)
                 vw2[j] = *(const uint2 *)(blk + swz(2 * D + 2 * (NJ * n + j) + (g4 >> 1)) * 16 + 8 * (g4 & 1));
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sc[r] = c[r];
+            for (int r = 0; r < 4; ++r) sc[r] = kTwo ? c[r] + dpp<kRowRor8>(c[r]) : c[r];
         }
         if constexpr (MASKED) {
 #pragma unroll
@@ -467,7 +485,9 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
                 }
             }
         }
-        const uint2 pb = make_uint2(pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]));
+        uint2 pb = make_uint2(pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]));
+        if constexpr (kTwo)
+            pb = make_uint2(bf16x2_rest(pv[0], pv[1], rest ? pb.x : 0u), bf16x2_rest(pv[2], pv[3], rest ? pb.y : 0u));
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
             if constexpr (F8)
@@ -562,7 +582,7 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
             const float *x = (const float *)&ring[q][0][0] + h * D + d;
             l = fmaf(sL[q][h], wq, l);
 #pragma unroll
-            for (int r = 0; r < VD; ++r) o[r] = fmaf(wq, x[r], o[r]);
+            for (int r = 0; r < VD; ++r) o[r] = fmaf(wq, kTwo ? x[r] + x[8 * D + r] : x[r], o[r]);
         }
         if (a.n_split == 1) {
             const float inv = 1.f / l;

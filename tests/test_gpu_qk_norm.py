@@ -189,3 +189,40 @@ def test_refused_while_the_current_stream_is_captured():
         g.replay()
         torch.cuda.synchronize()
     assert bool((x == 3).all())
+
+
+@pytest.mark.parametrize("fused", [False, True])
+@pytest.mark.parametrize("hq,hkv", [(8, 1), (8, 2), (4, 4)])
+def test_fp8_decode_is_off_by_its_outputs_rounding(hq, hkv, fused):
+    """The stored rows are exact operands, queries and probabilities have two bf16
+    terms (2^-16 and less of theirs): what is left is the output's rounding, of
+    which half a step is 2^-8 of values of [1, 2) and less, evenly spread: 2^-8 / sqrt(3)
+    in rms, were all of them at the lower end, and 2^-13 for everything else (queries
+    in one term would add as much again as the outputs' rounding, 0.0024 together with it
+    the least, probabilities in one the same)."""
+    d, n, layers = 128, 150, 1
+    pool = make_pool(n_layers=layers, hq=hq, hkv=hkv, d=d, S=4, W=200, cmax=n, max_sessions=1, n_blocks=23, dtype="fp8")
+    w = _weights(layers, d)
+    pool.set_qk_norm(*w)
+    o = wa.OracleSession(hq, hkv, d, 4, 200, n_layers=layers, kv_quant="fp8_e4m3")
+    o.qk_norm = (*w, 1e-6)
+    gen, sid, err, size = torch.Generator(device="cuda").manual_seed(hq), pool.session_open(), [], []
+    for t in [n] + [1] * 12:
+        q, k, v = (torch.randn((t, h, d), generator=gen, device="cuda").to(torch.bfloat16) for h in (hq, hkv, hkv))
+        out = torch.empty_like(q)
+        pool.plan_begin([sid], [t])
+        if t == 1 and fused:
+            pool.attend_decode_append(0, k, v, q, out)
+        else:
+            pool.frame_append_kv(0, k, v)
+            (pool.attend_decode if t == 1 else pool.attend_chunk_prefill)(0, q, out)
+        pool.plan_commit()
+        o.begin(t)
+        ref = o.layer_step(0, *(f64(x) for x in (q, k, v)))[0]
+        o.commit()
+        if t == 1:
+            err.append(f64(out) - ref)
+            size.append(ref)
+    rms = np.sqrt(np.mean(np.square(err)) / np.mean(np.square(size)))
+    say(f"fp8 {hq}/{hkv} fused {fused}: {rms:.5f}")
+    assert rms <= 2.0 ** -8 / np.sqrt(3) + 2.0 ** -13
