@@ -266,6 +266,7 @@ class Pool:
         self.required_bytes = nbytes.value
         self.kv = kv
         self.states = None  # of the linear layers: set_linear
+        self._linear_io = None  # their rows' torch dtype
         h = C.c_void_p()
         st = self.lib.mtn_pool_create(C.byref(self.cfg), _ptr(kv) if kv is not None else None,
                                       C.c_size_t(kv.numel() * kv.element_size() if kv is not None else 0),
@@ -410,6 +411,9 @@ class Pool:
         size = C.c_size_t(states.numel() * states.element_size() if states is not None else 0)
         self._check(self.lib.mtn_pool_set_linear(self.h, C.byref(cfg), _ptr(states), size), where)
         self.states = states
+        if states is not None:
+            import torch
+            self._linear_io = torch.float32 if dtype == "f32" else torch.bfloat16
 
     def clear_linear(self) -> None:
         """Take the linear layers away; the pool then holds their states no longer."""
@@ -429,6 +433,13 @@ class Pool:
         return self.states[sid, self.state_slot(sid)]
 
     def attend_linear(self, layer, q, k, v, out, stream=None) -> None:
+        """One linear layer of the open plan (mtn_attend_linear): contiguous device
+        tensors of the linear layers' dtype, q and out [T][Hq][D], k and v [T][Hkv][D]."""
+        if self._linear_io is not None:
+            for t in (q, k, v, out):
+                if t is not None and not (t.dtype == self._linear_io and t.is_cuda and t.is_contiguous()):
+                    raise MtnError(MTN_ERR_INVALID_ARG, "attend_linear", "rows: not a contiguous device tensor of the "
+                                   "linear layers' dtype")
         self._check(self.lib.mtn_attend_linear(self.h, layer, _ptr(q), _ptr(k), _ptr(v), _ptr(out),
                                                _stream(stream)), "attend_linear")
 

@@ -318,3 +318,78 @@ def test_single_tokens_decay_without_drift(a):
     say(f"a {a}: mean relative error {rel.mean():.2e}")
     assert abs(rel.mean()) <= 6 * 2.0 ** -24 * np.sqrt(2 * n / (3 * d * d)) + n * 2.0 ** -48
     assert np.abs(rel).max() <= 2 * n * 2.0 ** -24
+
+
+def test_refused_calls_change_nothing():
+    x = Linear("bf16", 4, 2, 64, n=2, layers=2, cmax=40)
+    x.step([5, 9])
+    bad, n = [], 40
+    rows = x.rows(n)
+    q, k, v = (r[0].cuda() for r in rows)
+    out = torch.full_like(q, 7.0)
+    pool, sides = x.pool, torch.cuda.Stream()
+
+    def code(fn, *args, **kw):
+        try:
+            fn(*args, **kw)
+            return 0
+        except mtn.MtnError as e:
+            return e.code
+    bad.append(code(pool.attend_linear, 0, q, k, v, out) == mtn.MTN_ERR_BAD_STATE)  # no plan
+    x.plan(x.sids, [39, 1])
+    bad.append(code(pool.plan_commit) == mtn.MTN_ERR_BAD_STATE)  # no linear layer yet
+    strided = torch.cat([q, q], 2)[..., :64]
+    shifted = torch.empty(q.numel() + 8, dtype=q.dtype, device="cuda")[1:1 + q.numel()].view_as(q)
+    for args in ((2, q, k, v, out), (-1, q, k, v, out), (0, None, k, v, out), (0, q, None, v, out),
+                 (0, q, k, None, out), (0, q, k, v, None), (0, q.float(), k, v, out), (0, strided, k, v, out),
+                 (0, q, k.cpu(), v, out), (0, q, k, v, shifted)):
+        bad.append(code(pool.attend_linear, *args) == mtn.MTN_ERR_INVALID_ARG)
+    bad.append(code(pool.attend_linear, 0, q, k, v, out, stream=sides.cuda_stream) == mtn.MTN_ERR_INVALID_ARG)
+    assert all(bad), bad
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())
+    pool.attend_linear(0, q, k, v, out)
+    assert code(pool.attend_linear, 0, q, k, v, out) == mtn.MTN_ERR_BAD_STATE  # again
+    assert code(pool.plan_commit) == mtn.MTN_ERR_BAD_STATE  # the other layer
+    pool.plan_abort()
+    for s in x.sids:
+        x.check_state(s)
+    x.step([39, 1], rows=rows)
+
+
+def test_states_that_set_linear_refuses():
+    x = Linear("bf16", 2, 2, 64, n=1)
+    shape = tuple(x.states.shape)
+    for states in (None, torch.zeros(shape, dtype=torch.bfloat16, device="cuda"), torch.zeros(shape),
+                   torch.zeros(shape[:-1] + (shape[-1] * 2,), device="cuda")[..., ::2],
+                   torch.zeros((2,) + shape[1:], device="cuda")):
+        with pytest.raises(mtn.MtnError) as e:
+            x.pool.set_linear(n_layers=1, n_q_heads=2, n_kv_heads=2, head_dim=64, dtype="bf16",
+                              log_decay=x.log_decay, states=states)
+        assert e.value.code == mtn.MTN_ERR_INVALID_ARG
+    x.step([9])
+    x.step([1])
+
+
+def test_states_past_2_to_the_31_elements():
+    """1100 sessions of 2 x 2 x 32 states; the last ones lie past 2^31 elements."""
+    n = 1100
+    x = Linear("bf16", 32, 32, 128, n=n, layers=2, cmax=16)
+    assert x.states.numel() > 2 ** 31
+    last = x.sids[-2:]
+    assert last == [n - 2, n - 1]
+    for n_tok in ([16, 3], [1, 1], [7, 1]):
+        x.step(n_tok, last)
+    x.step([2], x.sids[:1])
+
+
+def test_a_resized_pool_keeps_the_states():
+    x = Linear("bf16", 2, 2, 64, n=2, cmax=32)
+    x.step([20, 5])
+    kw = dict(n_layers=1, n_q_heads=1, n_kv_heads=1, head_dim=64, n_sink=0, window=32, max_chunk=32,
+              max_sessions=2, n_blocks=16, dtype="bf16")
+    x.pool.resize(16, torch.empty(mtn.Pool.required(**kw), dtype=torch.uint8, device="cuda"))
+    for s in x.sids:
+        x.check_state(s)
+    x.step([1, 1])
+    x.step([9, 32])
