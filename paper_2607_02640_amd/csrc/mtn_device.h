@@ -235,7 +235,7 @@ __device__ __forceinline__ void rope_split_f32(uint4 &x, uint4 &y, bool upper) {
 //
 // Several kernels store keys (append, decode and prefill with the append fused), and
 // their bytes agree: each adds a key's squares in one order, a tree over the bits
-// of the dim, D/2 first, then 1, 2, 4, .. (row_square: the pair of dims i and i + D/2 of
+// of the dim, D/2 first, then 1, 2, 4, .. (wave_norm_factor: the pair of dims i and i + D/2 of
 // lane i, then the lanes), in ordinary products and sums.
 struct NormView {
     const float *q, *k;  // weights in the order of the kernels' dims
