@@ -234,7 +234,7 @@ def _stream(stream) -> Optional[int]:
     if torch.cuda.is_initialized():
         # what current_stream().cuda_stream returns, without the Stream object, which
         # took half of a call's time on the host (3.4 of 6.6 us)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     if torch.cuda.is_available():
         return torch.cuda.current_stream().cuda_stream
     return None
@@ -435,13 +435,16 @@ class Pool:
     def attend_linear(self, layer, q, k, v, out, stream=None) -> None:
         """One linear layer of the open plan (mtn_attend_linear): contiguous device
         tensors of the linear layers' dtype, q and out [T][Hq][D], k and v [T][Hkv][D]."""
-        if self._linear_io is not None:
-            for t in (q, k, v, out):
-                if t is not None and not (t.dtype == self._linear_io and t.is_cuda and t.is_contiguous()):
-                    raise MtnError(MTN_ERR_INVALID_ARG, "attend_linear", "rows: not a contiguous device tensor of the "
-                                   "linear layers' dtype")
-        self._check(self.lib.mtn_attend_linear(self.h, layer, _ptr(q), _ptr(k), _ptr(v), _ptr(out),
-                                               _stream(stream)), "attend_linear")
+        io, rows = self._linear_io, []
+        for t in (q, k, v, out):
+            if t is None:
+                rows.append(None)
+                continue
+            if io is not None and not (t.dtype == io and t.is_contiguous() and t.is_cuda):
+                raise MtnError(MTN_ERR_INVALID_ARG, "attend_linear", "rows: not a contiguous device tensor of the "
+                               "linear layers' dtype")
+            rows.append(t.data_ptr())
+        self._check(self.lib.mtn_attend_linear(self.h, layer, *rows, _stream(stream)), "attend_linear")
 
     def set_decode_kernel(self, kind: int) -> None:
         """0 = by shape, 1 = vector kernel, 2 = matrix-core kernel."""
