@@ -136,7 +136,8 @@ struct mtn_pool {
     bool lin_split = false;           // ... some sequence is cut into segments
     int32_t lin_max = 0;              // ... tokens of the longest item
     float *lin_states = nullptr;      // caller's
-    float *d_lin_decay = nullptr;     // [3][n_layers][n_kv_heads]: log2, then e^log_decay in two terms
+    // [n_layers][n_kv_heads]: log2 of the decay, then its powers, as floats [.][.][kLinDecays]
+    double *d_lin_decay = nullptr;
     float *d_lin_seg = nullptr;       // segments' states
     int64_t lin_seg_cap = 0;          // ... of so many (segment, KV head) pairs
     int32_t *d_lin_items = nullptr;   // in d_meta
@@ -1658,7 +1659,7 @@ mtn_status mtn_pool_set_linear(mtn_pool *P, const mtn_linear_config *cfg, void *
         if (!P) return MTN_ERR_INVALID_ARG;
         if (mtn_status st = check_reform(P)) return st;
         mtn_linear_config c = {};
-        std::vector<float> decays;
+        std::vector<double> decays;
         if (cfg) {
             c = *cfg;
             size_t need = 0;
@@ -1667,20 +1668,26 @@ mtn_status mtn_pool_set_linear(mtn_pool *P, const mtn_linear_config *cfg, void *
                 return fail(P, MTN_ERR_INVALID_ARG, "null, misaligned or small state buffer");
             if (!c.log_decay) return fail(P, MTN_ERR_INVALID_ARG, "null log_decay");
             const size_t n = (size_t)c.n_layers * c.n_kv_heads;
-            decays.resize(3 * n);
+            std::vector<float> powers(n * kLinDecays);
+            decays.resize(n + powers.size() / 2);
             for (size_t i = 0; i < n; ++i) {
                 if (!(c.log_decay[i] <= 0.f) || !std::isfinite(c.log_decay[i]))
                     return fail(P, MTN_ERR_INVALID_ARG, "log_decay above 0 or not finite");
-                decays[i] = std::max((float)(c.log_decay[i] * 1.4426950408889634), -3.0e38f);
-                const double x = std::exp((double)c.log_decay[i]);
-                decays[n + i] = (float)x;
-                decays[2 * n + i] = (float)(x - decays[n + i]);
+                decays[i] = c.log_decay[i] * 1.4426950408889634;
+                float *const p = &powers[i * kLinDecays], *const rest = p + kLinTile + 1;
+                for (int m = 0; m <= kLinTile; ++m) {
+                    const double x = std::exp(m * (double)c.log_decay[i]);
+                    p[m] = (float)x;
+                    rest[m] = (float)(x - p[m]);
+                }
             }
+            std::memcpy(&decays[n], powers.data(), sizeof(float) * powers.size());
             if (c.scale == 0.f) c.scale = (float)(1.0 / std::sqrt((double)c.head_dim));
         }
         c.log_decay = nullptr;
         P->lin_done.reserve((size_t)c.n_layers);
-        float *decay = nullptr, *seg = nullptr;
+        double *decay = nullptr;
+        float *seg = nullptr;
         int64_t cap = 0;
         if (!P->host_only) {
             // new buffers before the old ones go; a capture under way on another stream
@@ -1694,10 +1701,10 @@ mtn_status mtn_pool_set_linear(mtn_pool *P, const mtn_linear_config *cfg, void *
             if (e == hipSuccess) e = hipSetDevice(P->device);
             if (e == hipSuccess && cfg) {
                 cap = (int64_t)kLinSegUnits * P->n_cu;
-                e = hipMalloc(&decay, sizeof(float) * decays.size());
+                e = hipMalloc(&decay, sizeof(double) * decays.size());
                 if (e == hipSuccess) e = hipMalloc(&seg, sizeof(float) * (size_t)cap * c.head_dim * c.head_dim);
                 if (e == hipSuccess)
-                    e = hipMemcpyAsync(decay, decays.data(), sizeof(float) * decays.size(), hipMemcpyHostToDevice,
+                    e = hipMemcpyAsync(decay, decays.data(), sizeof(double) * decays.size(), hipMemcpyHostToDevice,
                                        (hipStream_t)last);
             }
             const hipError_t e2 = hipStreamSynchronize((hipStream_t)last);
@@ -2056,7 +2063,8 @@ mtn_status mtn_attend_linear(mtn_pool *P, int32_t layer, const void *q, const vo
         a.slot_stride = c.n_layers * per;
         a.seg = P->d_lin_seg;
         a.log2_decay = P->d_lin_decay + (size_t)layer * c.n_kv_heads;
-        for (int i = 0; i < 2; ++i) a.decay[i] = a.log2_decay + (size_t)(i + 1) * c.n_layers * c.n_kv_heads;
+        a.decay = (const float *)(P->d_lin_decay + (size_t)c.n_layers * c.n_kv_heads) +
+                  (size_t)layer * c.n_kv_heads * kLinDecays;
         a.scale = c.scale;
         a.hq = c.n_q_heads;
         a.hkv = c.n_kv_heads;

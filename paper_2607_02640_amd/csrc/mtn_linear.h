@@ -8,10 +8,13 @@ namespace mtn {
 // One sequence of a plan, or one segment of it: {first io row, tokens, state slot
 // (2 * session + which of its two), with kLinFresh where the session holds no
 // token yet, segment | segments << 16}.  A sequence's segments follow one another;
-// all but its last hold a multiple of kLinTile tokens.
+// all but its last hold the same multiple of kLinTile tokens.
 constexpr int kLinItem = 4;
 constexpr int32_t kLinFresh = 1 << 30;
 constexpr int kLinTile = 64;
+// e^(m log_decay), m = 0 .. kLinTile, in two fp32 terms: the larger of each, then
+// what those leave
+constexpr int kLinDecays = 2 * (kLinTile + 1);
 constexpr int kLinMaxSeg = 1024;  // segments of a plan that cuts sequences, at most
 
 struct LinArgs {
@@ -21,8 +24,8 @@ struct LinArgs {
     float *state;             // the layer's states in slot 0: [Hkv][value D][key D]
     int64_t slot_stride;      // floats from a slot to the next
     float *seg;               // segments' states [item][Hkv][D][D]
-    const float *log2_decay;  // device [Hkv]
-    const float *decay[2];    // device [Hkv]: e^log_decay in two terms
+    const double *log2_decay;  // device [Hkv]
+    const float *decay;       // device [Hkv][kLinDecays]
     float scale;
     int32_t hq, hkv, d, n_items;
     int32_t parts;            // chunk form: workgroups that share a KV head's query heads
