@@ -2093,7 +2093,11 @@ __global__ __launch_bounds__(64 * kPfWaves) void k_prefill_mfma(PfArgs pa) {
                         }
                         v = make_uint4(v.x & vm[0], v.y & vm[1], v.z & vm[2], v.w & vm[3]);
                         f32x4_t t = mfma16x16x32(v, pb, acc[i][dt]);
-                        if constexpr (kTwo) t = mfma16x16x32(v, p_rest(w, pb), t);
+                        if constexpr (kTwo) {  // (an infinite sum is whole without the second term)
+                            const f32x4_t u = mfma16x16x32(v, p_rest(w, pb), t);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) t[e] = fabsf(t[e]) < INFINITY ? u[e] : t[e];
+                        }
 #pragma unroll
                         for (int e = 0; e < 4; ++e) acc[i][dt][e] = mine ? t[e] : acc[i][dt][e];
                     }

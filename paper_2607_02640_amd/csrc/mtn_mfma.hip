@@ -39,6 +39,18 @@ __device__ __forceinline__ uint32_t f8_bf16x2(uint32_t w) {
 __device__ __forceinline__ float f8_scale(uint32_t w, int r) {
     return __uint_as_float(((w >> (8 * r)) & 0xFFu) << 23);
 }
+// A sum of two terms' products, lo of what the rounding of hi's operand leaves: where
+// a factor is infinite, that remainder's sign or zero makes lo anything, and hi alone
+// is the sum.
+__device__ __forceinline__ float two_terms(float hi, float lo) { return fabsf(hi) < INFINITY ? hi + lo : hi; }
+// ... hi in lanes 0 .. 7 of a row, its lo in lanes 8 .. 15: the sum in both
+__device__ __forceinline__ float two_columns(float c) {
+    const int x = __builtin_bit_cast(int, c);
+    // (lanes 8 .. 15 take lane - 8, the others keep theirs)
+    const float hi = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(x, x, kRowRor8, 0xf, 0xc, false));
+    const float sum = c + dpp<kRowRor8>(c);
+    return fabsf(hi) < INFINITY ? sum : hi;
+}
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 // The 16-key PV product: lane (m, g4) brings the 4 keys 4 g4 .. 4 g4 + 3 of
 // both operands (the 16x16x16 MFMA's k slice of the lane).
@@ -420,7 +432,7 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
             }
             vw[0] = w0.x; vw[1] = w0.y; vw[2] = w0.z; vw[3] = w0.w;
             vw[4] = w1.x; vw[5] = w1.y; vw[6] = w1.z; vw[7] = w1.w;
-            if constexpr (kTwo)
+            if constexpr (kTwo)  // (codes are finite or NaN; of an infinite query every score is not finite)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) c[r] += dpp<kRowRor8>(c[r]);
 #pragma unroll
@@ -433,7 +445,7 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
             for (int j = 0; j < NJ; ++j)
                 vw2[j] = *(const uint2 *)(blk + swz(2 * D + 2 * (NJ * n + j) + (g4 >> 1)) * 16 + 8 * (g4 & 1));
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sc[r] = kTwo ? c[r] + dpp<kRowRor8>(c[r]) : c[r];
+            for (int r = 0; r < 4; ++r) sc[r] = kTwo ? two_columns(c[r]) : c[r];
         }
         if constexpr (MASKED) {
 #pragma unroll
@@ -582,7 +594,7 @@ __global__ __launch_bounds__(64 * NG) void k_attn_mfma(AttnArgs a) {
             const float *x = (const float *)&ring[q][0][0] + h * D + d;
             l = fmaf(sL[q][h], wq, l);
 #pragma unroll
-            for (int r = 0; r < VD; ++r) o[r] = fmaf(wq, kTwo ? x[r] + x[8 * D + r] : x[r], o[r]);
+            for (int r = 0; r < VD; ++r) o[r] = fmaf(wq, kTwo ? two_terms(x[r], x[8 * D + r]) : x[r], o[r]);
         }
         if (a.n_split == 1) {
             const float inv = 1.f / l;
