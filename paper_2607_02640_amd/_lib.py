@@ -227,6 +227,13 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+def _whole_rows(t, n: int, per: int, d: int) -> bool:
+    """At least ``n`` rows of ``per`` elements, which are heads of ``d`` where the
+    shape says how a row is cut."""
+    cut = t.shape[-2:] if t.dim() > 2 else t.shape[1:]
+    return t.numel() >= n * per and tuple(cut) in ((per // d, d), (per,), ())
+
+
 def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream
@@ -266,7 +273,8 @@ class Pool:
         self.required_bytes = nbytes.value
         self.kv = kv
         self.states = None  # of the linear layers: set_linear
-        self._linear_io = None  # their rows' torch dtype
+        self._linear_rows = None  # their rows: torch dtype, device, elements of a query's and a KV row, head dim
+        self._plan_tokens = 0  # of the open plan
         h = C.c_void_p()
         st = self.lib.mtn_pool_create(C.byref(self.cfg), _ptr(kv) if kv is not None else None,
                                       C.c_size_t(kv.numel() * kv.element_size() if kv is not None else 0),
@@ -343,15 +351,19 @@ class Pool:
         self.required_bytes, self.kv = n.value, kv
 
     def plan_begin(self, sids, n_tok, stream=None) -> None:
-        st = self.lib.mtn_plan_begin(self.h, len(sids), _arr32(sids), _arr32(n_tok),
+        n_tok = _arr32(n_tok)
+        st = self.lib.mtn_plan_begin(self.h, len(sids), _arr32(sids), n_tok,
                                      None if self.host_only else _stream(stream))
         self._check(st, "plan_begin")
+        self._plan_tokens = sum(n_tok[:len(sids)])
 
     def plan_commit(self) -> None:
         self._check(self.lib.mtn_plan_commit(self.h), "plan_commit")
+        self._plan_tokens = 0
 
     def plan_abort(self) -> None:
         self._check(self.lib.mtn_plan_abort(self.h), "plan_abort")
+        self._plan_tokens = 0
 
     def _not_captured(self, where: str) -> None:
         if not self.host_only:
@@ -411,15 +423,17 @@ class Pool:
         size = C.c_size_t(states.numel() * states.element_size() if states is not None else 0)
         self._check(self.lib.mtn_pool_set_linear(self.h, C.byref(cfg), _ptr(states), size), where)
         self.states = states
+        self._linear_rows = None
         if states is not None:
             import torch
-            self._linear_io = torch.float32 if dtype == "f32" else torch.bfloat16
+            self._linear_rows = (torch.float32 if dtype == "f32" else torch.bfloat16, states.device,
+                                 n_q_heads * head_dim, n_kv_heads * head_dim, head_dim)
 
     def clear_linear(self) -> None:
         """Take the linear layers away; the pool then holds their states no longer."""
         self._not_captured("clear_linear")
         self._check(self.lib.mtn_pool_set_linear(self.h, None, None, C.c_size_t(0)), "clear_linear")
-        self.states = None
+        self.states = self._linear_rows = None
 
     def state_slot(self, sid: int) -> int:
         """Which of session ``sid``'s two slots of the states is the committed one."""
@@ -433,18 +447,23 @@ class Pool:
         return self.states[sid, self.state_slot(sid)]
 
     def attend_linear(self, layer, q, k, v, out, stream=None) -> None:
-        """One linear layer of the open plan (mtn_attend_linear): contiguous device
-        tensors of the linear layers' dtype, q and out [T][Hq][D], k and v [T][Hkv][D]."""
-        io, rows = self._linear_io, []
-        for t in (q, k, v, out):
-            if t is None:
-                rows.append(None)
-                continue
-            if io is not None and not (t.dtype == io and t.is_contiguous() and t.is_cuda):
-                raise MtnError(MTN_ERR_INVALID_ARG, "attend_linear", "rows: not a contiguous device tensor of the "
-                               "linear layers' dtype")
-            rows.append(t.data_ptr())
-        self._check(self.lib.mtn_attend_linear(self.h, layer, *rows, _stream(stream)), "attend_linear")
+        """One linear layer of the open plan (mtn_attend_linear): contiguous tensors of
+        the linear layers' dtype on the pool's device, q and out [T][Hq][D], k and v
+        [T][Hkv][D] or more rows (those behind the plan's are left alone)."""
+        ptrs = [None if t is None else t.data_ptr() for t in (q, k, v, out)]
+        if self._linear_rows is not None:
+            io, dev, per_q, per_kv, d = self._linear_rows
+            n = self._plan_tokens
+            for t, per in ((q, per_q), (k, per_kv), (v, per_kv), (out, per_q)):
+                if t is None:
+                    continue
+                if not (t.dtype == io and t.is_contiguous() and t.device == dev):
+                    raise MtnError(MTN_ERR_INVALID_ARG, "attend_linear", "rows: not a contiguous tensor of the linear "
+                                   "layers' dtype on the pool's device")
+                if n and t.numel() != n * per and not _whole_rows(t, n, per, d):
+                    raise MtnError(MTN_ERR_INVALID_ARG, "attend_linear",
+                                   f"rows {tuple(t.shape)}: not {n} rows of {per // d} x {d} elements or more")
+        self._check(self.lib.mtn_attend_linear(self.h, layer, *ptrs, _stream(stream)), "attend_linear")
 
     def set_decode_kernel(self, kind: int) -> None:
         """0 = by shape, 1 = vector kernel, 2 = matrix-core kernel."""
