@@ -240,8 +240,12 @@ def _stream(stream) -> Optional[int]:
     import torch
     if torch.cuda.is_initialized():
         # what current_stream().cuda_stream returns, without the Stream object, which
-        # took half of a call's time on the host (3.4 of 6.6 us)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        # took half of a call's time on the host (3.4 of 6.6 us); the names are torch's
+        # own, and a torch without them is asked the public way
+        try:
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        except AttributeError:
+            return torch.cuda.current_stream().cuda_stream
     if torch.cuda.is_available():
         return torch.cuda.current_stream().cuda_stream
     return None
