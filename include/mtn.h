@@ -275,8 +275,8 @@ mtn_status mtn_linear_required_bytes(const mtn_pool *pool, const mtn_linear_conf
  * tokens and no plan is open (MTN_ERR_BAD_STATE otherwise, or while the previous
  * plan's stream is being captured).  states_dev: device, 256-byte aligned, >=
  * mtn_linear_required_bytes, kept alive until the layers are taken away or the pool is
- * destroyed (host-only pools: may be NULL).  Allocates the segments' workspace (4 D^2
- * floats per compute unit; 67 MB on 256 at D = 128) and synchronises the stream of
+ * destroyed (host-only pools: may be NULL).  Allocates the segments' workspace (3 D^2
+ * floats per compute unit; 50 MB on 256 at D = 128) and synchronises the stream of
  * the previous plan.  Every plan then has to bring every linear layer too
  * (mtn_plan_commit: MTN_ERR_BAD_STATE otherwise), mtn_session_fork copies the state,
  * and mtn_frame_step, whose batch has no place for linear rows, is refused

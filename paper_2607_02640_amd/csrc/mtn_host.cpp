@@ -42,8 +42,6 @@ constexpr double kPfMinSavedF32 = 3.0;
 // timing classes: append, prefill, decode, the decode's merge, the prefill's merge,
 // the linear layers
 constexpr int kTimeClasses = 6;
-// segments' states that a pool with linear layers has room for, per compute unit
-constexpr int kLinSegUnits = 4;
 constexpr size_t kZeroPage = 2 * kBlock * 128 * 4;  // 16 KiB
 
 // Lowest-free-first block allocator over a bitmap (bit set = free).
@@ -139,7 +137,6 @@ struct mtn_pool {
     // [n_layers][n_kv_heads]: log2 of the decay, then its powers, as floats [.][.][kLinDecays]
     double *d_lin_decay = nullptr;
     float *d_lin_seg = nullptr;       // segments' states
-    int64_t lin_seg_cap = 0;          // ... of so many (segment, KV head) pairs
     int32_t *d_lin_items = nullptr;   // in d_meta
     int64_t lin_launch = 0;           // launches and milliseconds that
     double lin_ms = 0.0;              // mtn_pool_kernel_times last found
@@ -667,23 +664,8 @@ void plan_linear(mtn_pool *P) {
     P->lin_split = false;
     P->lin_max = 0;
     if (!P->lin.n_layers) return;
-    const int64_t hkv = P->lin.n_kv_heads;
-    int64_t len = P->max_ntok;  // tokens of a segment
-    if (!P->all_single && P->n_cu > 0 && P->n_seq * hkv < P->n_cu) {
-        // Two workgroups a CU, half of that where a KV head's query heads can share
-        // one's work (launch_linear_chunk), of at least two tiles.  Each segment's
-        // state is written, scanned and read, 4 D^2 floats of traffic (32 heads of
-        // 8192 tokens, D = 128: 8 segments 156 us, 12 151, 16 137, 24 159; 4 heads of
-        // G = 8, in two parts: 16 segments 94 us, 32 77, 64 78).
-        const int64_t want = std::max<int64_t>((P->lin.n_q_heads > hkv ? 1 : 2) * P->n_cu / hkv, 1);
-        len = std::max<int64_t>(ceil_div(ceil_div(P->T, want), kLinTile) * kLinTile, 2 * kLinTile);
-        auto segments = [&] {
-            int64_t m = 0;
-            for (int32_t i = 0; i < P->n_seq; ++i) m += ceil_div(P->seq_ntok[i], len);
-            return m;
-        };
-        while (segments() * hkv > P->lin_seg_cap || segments() > P->n_seq + kLinMaxSeg) len += kLinTile;
-    }
+    int64_t len = P->all_single ? 0 : linear_segment(P->n_seq, P->T, P->lin.n_q_heads, P->lin.n_kv_heads, P->n_cu);
+    if (!len) len = P->max_ntok;
     for (int32_t i = 0; i < P->n_seq; ++i) {
         const int32_t sid = P->seq_sid[i], nt = P->seq_ntok[i];
         const int32_t nseg = (int32_t)ceil_div(nt, len);
@@ -1688,7 +1670,6 @@ mtn_status mtn_pool_set_linear(mtn_pool *P, const mtn_linear_config *cfg, void *
         P->lin_done.reserve((size_t)c.n_layers);
         double *decay = nullptr;
         float *seg = nullptr;
-        int64_t cap = 0;
         if (!P->host_only) {
             // new buffers before the old ones go; a capture under way on another stream
             // is left alone
@@ -1700,9 +1681,9 @@ mtn_status mtn_pool_set_linear(mtn_pool *P, const mtn_linear_config *cfg, void *
             hipError_t e = hipGetDevice(&dev);
             if (e == hipSuccess) e = hipSetDevice(P->device);
             if (e == hipSuccess && cfg) {
-                cap = (int64_t)kLinSegUnits * P->n_cu;
+                const size_t cap = (size_t)kLinSegUnits * P->n_cu;
                 e = hipMalloc(&decay, sizeof(double) * decays.size());
-                if (e == hipSuccess) e = hipMalloc(&seg, sizeof(float) * (size_t)cap * c.head_dim * c.head_dim);
+                if (e == hipSuccess) e = hipMalloc(&seg, sizeof(float) * cap * c.head_dim * c.head_dim);
                 if (e == hipSuccess)
                     e = hipMemcpyAsync(decay, decays.data(), sizeof(double) * decays.size(), hipMemcpyHostToDevice,
                                        (hipStream_t)last);
@@ -1724,7 +1705,6 @@ mtn_status mtn_pool_set_linear(mtn_pool *P, const mtn_linear_config *cfg, void *
         P->lin_states = cfg ? (float *)states_dev : nullptr;
         P->d_lin_decay = decay;
         P->d_lin_seg = seg;
-        P->lin_seg_cap = cap;
         return MTN_OK;
     });
 }

@@ -1,5 +1,7 @@
 // Internal launch interface of the linear-attention layers (mtn_linear.hip).
 #pragma once
+#include <algorithm>
+
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -30,6 +32,23 @@ struct LinArgs {
     int32_t hq, hkv, d, n_items;
     int32_t parts;            // chunk form: workgroups that share a KV head's query heads
 };
+
+// Tokens of a segment of a plan of n_seq sequences and n_tok tokens; 0: nothing is cut.
+// Sequences are cut where they leave compute units idle: two workgroups a CU, half of that
+// where a KV head's query heads can share one's work (linear_parts), of at least two
+// tiles.  Each segment's state is written, scanned and read, 4 D^2 floats of
+// traffic (32 heads of 8192 tokens, D = 128: 8 segments 156 us, 12 151, 16 137, 24 159;
+// 4 heads of G = 8, in two parts: 16 segments 94 us, 32 77, 64 78).
+inline int64_t linear_segment(int64_t n_seq, int64_t n_tok, int64_t hq, int64_t hkv, int64_t n_cu) {
+    if (n_cu < 1 || n_seq * hkv >= n_cu) return 0;
+    const int64_t want = std::min<int64_t>((hq > hkv ? 1 : 2) * n_cu / hkv, kLinMaxSeg);
+    const int64_t len = (n_tok + want - 1) / want;
+    return std::max<int64_t>((len + kLinTile - 1) / kLinTile, 2) * kLinTile;
+}
+// (segment, KV head) pairs of such a plan, per compute unit, that it stays under: each
+// sequence adds one segment to n_tok / len <= want, n_seq + want segments in all, of
+// which n_seq hkv < n_cu and want hkv <= 2 n_cu pairs.
+constexpr int kLinSegUnits = 3;
 
 bool linear_supported(int dtype, int d, int g);
 // Plans of one token per sequence
