@@ -50,6 +50,27 @@ inline int64_t linear_segment(int64_t n_seq, int64_t n_tok, int64_t hq, int64_t 
 // which n_seq hkv < n_cu and want hkv <= 2 n_cu pairs.
 constexpr int kLinSegUnits = 3;
 
+// Tokens of a chunk workgroup's tiles: 32 take chunks up to 32 tokens and fp32.
+inline int linear_tile(int dtype, int max_tok) { return dtype == 1 && max_tok > 32 ? 64 : 32; }
+// Workgroups that share a KV head's query heads in the chunk form, each with the state,
+// where that fills the CUs: with a workgroup of eight waves each (tiles of 32), or two of
+// four (one session of 25 tokens, G = 4, 4 KV heads 14.9 us whole, 10.5 in four
+// parts; 32 sessions 16.6, 15.3 in two, 18.5 in four; 8192 tokens of G = 8, 4 KV
+// heads, 64 segments 90.3 whole, 77.7 in two, 89.3 in four).
+inline int linear_parts(int64_t units, int g, int tile, int n_cu) {
+    int parts = 1;
+    while (2 * parts * units <= (tile == 64 ? 2 : 1) * (int64_t)n_cu && g % (2 * parts) == 0) parts *= 2;
+    return parts;
+}
+// Workgroups that share the rows of a state in the single-token form, where states are
+// few (32 sessions, G = 4, 4 heads 9.7 us whole, 8.0 in four slices; 512 states of
+// G = 8 19.2 whole, 21.0 in two).
+inline int linear_slices(int64_t units, int d, int n_cu) {
+    int sl = 1;
+    while (sl < d / 32 && sl * units <= n_cu) sl *= 2;
+    return sl;
+}
+
 bool linear_supported(int dtype, int d, int g);
 // Plans of one token per sequence
 hipError_t launch_linear_decode(int dtype, const LinArgs &a, int n_cu, hipStream_t s);

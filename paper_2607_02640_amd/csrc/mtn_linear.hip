@@ -726,11 +726,7 @@ hipError_t launch_linear_decode(int dtype, const LinArgs &a, int n_cu, hipStream
                 hipLaunchKernelGGL((k_linear_decode<T, D, G, SL>), dim3((unsigned)(units * SL)), dim3(kLinThreads), 0,
                                    s, a);
             };
-            // rows of a state over several workgroups where states are few (32 sessions,
-            // G = 4, 4 heads 9.7 us whole, 8.0 in four slices; 512 states of G = 8 19.2
-            // whole, 21.0 in two)
-            int sl = 1;
-            while (sl < kMost && 2 * sl * units <= 2 * (int64_t)n_cu) sl *= 2;
+            const int sl = linear_slices(units, D, n_cu);
             if (sl == 1) return sliced(std::integral_constant<int, 1>{});
             if (sl == 2 || kMost == 2) return sliced(std::integral_constant<int, 2>{});
             sliced(std::integral_constant<int, kMost>{});
@@ -748,15 +744,8 @@ hipError_t launch_linear_chunk(int dtype, LinArgs a, int max_tok, bool split, in
     if (!linear_supported(dtype, a.d, a.hq / a.hkv) || a.n_items < 1 || (split && !a.seg)) return hipErrorInvalidValue;
     const int64_t units = (int64_t)a.n_items * a.hkv;
     if (units > (split ? 65535 : INT32_MAX)) return hipErrorInvalidValue;  // (the scan's second grid dimension)
-    // 32-token tiles take chunks up to 32 tokens and fp32; the query heads of a KV head
-    // go to several workgroups, each with the state, where that fills the CUs: with a
-    // workgroup of eight waves each, or two of four (one session of 25 tokens, G = 4,
-    // 4 KV heads 14.9 us whole, 10.5 in four parts; 32 sessions 16.6, 15.3 in two, 18.5
-    // in four; 8192 tokens of G = 8, 4 KV heads, 64 segments 90.3 whole, 77.7 in two,
-    // 89.3 in four).
-    const int tile = dtype == 1 && max_tok > 32 ? 64 : 32;
-    a.parts = 1;
-    while (2 * a.parts * units <= (tile == 64 ? 2 : 1) * (int64_t)n_cu && a.hq / a.hkv % (2 * a.parts) == 0) a.parts *= 2;
+    const int tile = linear_tile(dtype, max_tok);
+    a.parts = linear_parts(units, a.hq / a.hkv, tile, n_cu);
     return by_shape(dtype, a.d, [&](auto dc, auto elt) {
         constexpr int D = decltype(dc)::value;
         using T = decltype(elt);
