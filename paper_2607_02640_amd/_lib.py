@@ -227,17 +227,16 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
-def _whole_rows(t, n: int, per: int, d: int) -> bool:
-    """At least ``n`` rows of ``per`` elements, which are heads of ``d`` where the
-    shape says how a row is cut."""
-    cut = t.shape[-2:] if t.dim() > 2 else t.shape[1:]
-    return t.numel() >= n * per and tuple(cut) in ((per // d, d), (per,), ())
+_torch = None  # once _stream has been asked
 
 
 def _stream(stream) -> Optional[int]:
+    global _torch
     if stream is not None:
         return stream
-    import torch
+    if _torch is None:
+        import torch as _torch
+    torch = _torch
     if torch.cuda.is_initialized():
         # what current_stream().cuda_stream returns, without the Stream object, which
         # took half of a call's time on the host (3.4 of 6.6 us); the names are torch's
@@ -277,7 +276,8 @@ class Pool:
         self.required_bytes = nbytes.value
         self.kv = kv
         self.states = None  # of the linear layers: set_linear
-        self._linear_rows = None  # their rows: torch dtype, device, elements of a query's and a KV row, head dim
+        # their rows: torch dtype, device's index, elements of a query's and a KV row, device, head dim
+        self._linear_rows = None
         self._plan_tokens = 0  # of the open plan
         h = C.c_void_p()
         st = self.lib.mtn_pool_create(C.byref(self.cfg), _ptr(kv) if kv is not None else None,
@@ -430,8 +430,9 @@ class Pool:
         self._linear_rows = None
         if states is not None:
             import torch
-            self._linear_rows = (torch.float32 if dtype == "f32" else torch.bfloat16, states.device,
-                                 n_q_heads * head_dim, n_kv_heads * head_dim, head_dim)
+            self._linear_rows = (torch.float32 if dtype == "f32" else torch.bfloat16,
+                                 None if self.host_only else states.get_device(), n_q_heads * head_dim,
+                                 n_kv_heads * head_dim, states.device, head_dim)
 
     def clear_linear(self) -> None:
         """Take the linear layers away; the pool then holds their states no longer."""
@@ -454,20 +455,32 @@ class Pool:
         """One linear layer of the open plan (mtn_attend_linear): contiguous tensors of
         the linear layers' dtype on the pool's device, q and out [T][Hq][D], k and v
         [T][Hkv][D] or more rows (those behind the plan's are left alone)."""
-        ptrs = [None if t is None else t.data_ptr() for t in (q, k, v, out)]
         if self._linear_rows is not None:
-            io, dev, per_q, per_kv, d = self._linear_rows
-            n = self._plan_tokens
-            for t, per in ((q, per_q), (k, per_kv), (v, per_kv), (out, per_q)):
-                if t is None:
-                    continue
-                if not (t.dtype == io and t.is_contiguous() and t.device == dev):
-                    raise MtnError(MTN_ERR_INVALID_ARG, "attend_linear", "rows: not a contiguous tensor of the linear "
-                                   "layers' dtype on the pool's device")
-                if n and t.numel() != n * per and not _whole_rows(t, n, per, d):
-                    raise MtnError(MTN_ERR_INVALID_ARG, "attend_linear",
-                                   f"rows {tuple(t.shape)}: not {n} rows of {per // d} x {d} elements or more")
-        self._check(self.lib.mtn_attend_linear(self.h, layer, *ptrs, _stream(stream)), "attend_linear")
+            io, dev, per_q, per_kv, *_ = self._linear_rows
+            nq, nkv = self._plan_tokens * per_q, self._plan_tokens * per_kv
+            # (one pass over what nearly every call brings; a layer's call is 5 us of host time)
+            for t, n, per in (q, nq, per_q), (k, nkv, per_kv), (v, nkv, per_kv), (out, nq, per_q):
+                if t is None or not (t.dtype is io and t.numel() == n and t.get_device() == dev and t.is_contiguous()):
+                    self._check_linear_rows(t, n, per)
+        st = self.lib.mtn_attend_linear(self.h, layer, None if q is None else q.data_ptr(),
+                                        None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
+                                        None if out is None else out.data_ptr(), _stream(stream))
+        if st:
+            self._check(st, "attend_linear")
+
+    def _check_linear_rows(self, t, n: int, per: int) -> None:
+        """At least ``n`` elements in rows of ``per``, which are heads of D where the
+        shape says how a row is cut; the library refuses None."""
+        io, _, _, _, device, d = self._linear_rows
+        if t is None:
+            return
+        if not (t.dtype == io and t.device == device and t.is_contiguous()):
+            raise MtnError(MTN_ERR_INVALID_ARG, "attend_linear", "rows: not a contiguous tensor of the linear "
+                           "layers' dtype on the pool's device")
+        cut = tuple(t.shape[-2:] if t.dim() > 2 else t.shape[1:])
+        if n and not (t.numel() >= n and cut in ((per // d, d), (per,), ())):
+            raise MtnError(MTN_ERR_INVALID_ARG, "attend_linear",
+                           f"rows {tuple(t.shape)}: not {n // per} rows of {per // d} x {d} elements or more")
 
     def set_decode_kernel(self, kind: int) -> None:
         """0 = by shape, 1 = vector kernel, 2 = matrix-core kernel."""

@@ -79,3 +79,11 @@ def test_rows_on_another_device_are_refused():
     pool, sids = _pool()
     pool.plan_begin(sids, [1, 1])
     assert _code(pool, [torch.empty_like(r, device="meta") for r in _rows(2)]) == mtn.MTN_ERR_INVALID_ARG
+
+
+def test_one_tensor_in_two_places_is_held_against_both():
+    pool, sids = _pool()
+    pool.plan_begin(sids, [3, 2])
+    q, k, v, out = _rows(5)
+    assert _code(pool, (q, q, v, out)) == mtn.MTN_ERR_INVALID_ARG  # four heads where there are two
+    assert _code(pool, (q, k, k, out)) == mtn.MTN_ERR_BAD_STATE
