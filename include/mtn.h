@@ -240,14 +240,15 @@ typedef struct {
 mtn_status mtn_pool_set_qk_norm(mtn_pool *pool, const mtn_qk_norm_config *norm);
 
 /*
- * Linear-attention layers beside the windowed ones (hybrid models; the other way to
- * bound what a session keeps, Metronome §4.1).  A linear layer keeps one matrix S of
+ * Linear-attention layers beside the windowed ones (hybrid models; a state of fixed
+ * size bounds what a session keeps as a window does).  A linear layer keeps one matrix S of
  * value dims by key dims in fp32 per session and KV head, shared by the G = Hq / Hkv
  * query heads of the KV head.  Token t of a session takes
  *   S_t = exp(log_decay) S_(t-1) + v_t k_t^T,    out_t = scale * S_t q_t
  * with S = 0 before a session's first token; q and k are taken as they are (neither
  * normed nor rotated).  Products and sums are fp32 (bf16 scores and states that
- * only make a bf16 output count to 16 bits), outputs are rounded once, states
+ * only make a bf16 output count to 16 bits; the decay of a state to 48, so that
+ * states do not drift over long sessions), outputs are rounded once, states
  * never.  Elements that are not finite reach the outputs and states of their own and
  * later tokens of the session, where an infinity may read NaN, and no others.
  *

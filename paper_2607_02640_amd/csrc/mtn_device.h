@@ -224,10 +224,17 @@ __device__ __forceinline__ void rope_split_f32(uint4 &x, uint4 &y, bool upper) {
 // fp32 throughout, nothing is rounded to fewer bits between norm and rotation.  The
 // rows are in registers where they are rotated, so a norm moves no byte but its
 // weights; it costs the reduction over the lanes that share a row and the products,
-// before the first key is looked at: per launch 1.3 us of a lone session's decode
-// (G = 8, D = 128: 9.7 -> 11.0), 85.4 -> 87.4 us of 128 sessions' over 2052 keys, 133
-// -> 136 of their chunk prefill and 10.5 -> 11.9 of the append, 25.5 -> 29.6 of
-// 13 fp32 sessions' decode at G = 4 (whose lanes rotate every element 16 times).  A sum of
+// before the first key is looked at, and registers there: rows and weights are held
+// whole, which a decode kernel then keeps room for to its end.  In the third instances
+// k_attn_mfma takes 199 registers over fp8 blocks (125 in the first) and k_attn_i8 194
+// (128), two waves a SIMD where four fit, k_attn_valu<bf16, 128, 4> 299 (226), one
+// where two fit.  All there is to a norm, per launch of D = 128 over 2052 keys, first ->
+// third instance: decode of one bf16 session of G = 8 10.1 -> 12.1 us, of 128 85.5 ->
+// 88.4, of 256 of G = 4 (k_attn_valu) 341 -> 361; fp8 51.5 -> 53.3 and 178 -> 213, int8
+// 52.7 -> 56.4 and 182 -> 194; 13 fp32 sessions over 904 keys 25.6 -> 29.5 (their lanes rotate every
+// element 16 times).  Chunks of 25 tokens of those 128 and 256 sessions: bf16 139 ->
+// 139 and 424 -> 434, fp8 174 -> 228 and 526 -> 624 (the probabilities' second term),
+// int8 167 -> 173 and 531 -> 518; their bf16 append 10.8 -> 12.3 and 24.3 -> 28.1.  A sum of
 // squares past 2^120 is taken once more of elements times 2^-70, so that no row of
 // finite elements overflows it.  (In 64 bits, where nothing overflows and bf16
 // squares add without rounding, the append of 128 x 25 tokens of 4 heads took

@@ -2184,6 +2184,8 @@ hipError_t launch_valu_d(const AttnArgs &a, int G, hipStream_t s) {
     }
 }
 
+// (Of the first instance.  That of norms has more registers: half as many bf16
+// workgroups fit at G = 4 and 8, so a split of theirs may take two rounds.)
 template <typename T, int D, int G>
 int resident_t() {
     using DS = DecodeShape<G>;

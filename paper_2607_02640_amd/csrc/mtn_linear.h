@@ -37,8 +37,8 @@ struct LinArgs {
 // Sequences are cut where they leave compute units idle: two workgroups a CU, half of that
 // where a KV head's query heads can share one's work (linear_parts), of at least two
 // tiles.  Each segment's state is written, scanned and read, 4 D^2 floats of
-// traffic (32 heads of 8192 tokens, D = 128: 8 segments 156 us, 12 151, 16 137, 24 159;
-// 4 heads of G = 8, in two parts: 16 segments 94 us, 32 77, 64 78).
+// traffic (32 heads of 8192 tokens, D = 128: 8 segments 153 us, 12 147, 16 124, 24 149;
+// 4 heads of G = 8: 16 segments 103 us, 32 79, 64 72).
 inline int64_t linear_segment(int64_t n_seq, int64_t n_tok, int64_t hq, int64_t hkv, int64_t n_cu) {
     if (n_cu < 1 || n_seq * hkv >= n_cu) return 0;
     const int64_t want = std::min<int64_t>((hq > hkv ? 1 : 2) * n_cu / hkv, kLinMaxSeg);
@@ -54,17 +54,17 @@ constexpr int kLinSegUnits = 3;
 inline int linear_tile(int dtype, int max_tok) { return dtype == 1 && max_tok > 32 ? 64 : 32; }
 // Workgroups that share a KV head's query heads in the chunk form, each with the state,
 // where that fills the CUs: with a workgroup of eight waves each (tiles of 32), or two of
-// four (one session of 25 tokens, G = 4, 4 KV heads 14.9 us whole, 10.5 in four
-// parts; 32 sessions 16.6, 15.3 in two, 18.5 in four; 8192 tokens of G = 8, 4 KV
-// heads, 64 segments 90.3 whole, 77.7 in two, 89.3 in four).
+// four (one session of 25 tokens, G = 4, 4 KV heads 14.5 us whole, 11.0 in four
+// parts; 32 sessions 16.6, 15.2 in two, 18.9 in four; 8192 tokens of G = 8, 4 KV
+// heads, 64 segments 84.5 whole, 72.8 in two, 86.2 in four).
 inline int linear_parts(int64_t units, int g, int tile, int n_cu) {
     int parts = 1;
     while (2 * parts * units <= (tile == 64 ? 2 : 1) * (int64_t)n_cu && g % (2 * parts) == 0) parts *= 2;
     return parts;
 }
 // Workgroups that share the rows of a state in the single-token form, where states are
-// few (32 sessions, G = 4, 4 heads 9.7 us whole, 8.0 in four slices; 512 states of
-// G = 8 19.2 whole, 21.0 in two).
+// few (32 sessions, G = 4, 4 heads 9.0 us whole, 7.2 in four slices; 512 states of
+// G = 8 17.6 whole, 18.4 in two).
 inline int linear_slices(int64_t units, int d, int n_cu) {
     int sl = 1;
     while (sl < d / 32 && sl * units <= n_cu) sl *= 2;

@@ -20,7 +20,7 @@ constexpr int kLinThreads = 256;  // of the single-token form
 // Waves of a chunk workgroup with tiles of B tokens.  Four with 64-token tiles: at
 // eight, a wave's operands served half as many products, and its registers (128 for
 // two workgroups a CU) spilled in the loop (one prompt of 8192 tokens of 32 heads
-// 144 us, 137 with four).  With 32-token tiles eight at D = 128 end sooner where
+// 5 % longer than with four).  With 32-token tiles eight at D = 128 end sooner where
 // few workgroups run (32 sessions of 25 tokens, G = 4, 4 KV heads 16.5 us, four 18.0).
 constexpr int lin_waves(int d, int b) { return b == 64 ? 4 : d / 16; }
 

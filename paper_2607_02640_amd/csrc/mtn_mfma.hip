@@ -677,7 +677,8 @@ int resident_mfma_g() {
     // at split 4 against 37.7 at 2; 256 units: bf16 87.2 unsplit against 93.2
     // at split 2, fp8 53.7 at split 2 against 60.8 unsplit.  (With more
     // streams in flight the decode ran slower: deeper rings, more waves per
-    // unit, and fp8 split to fill the four workgroups its registers allow.)
+    // unit, and fp8 split to fill the four workgroups its registers allow.)  So many
+    // fit of every instance, also of the one of norms with its 199 registers.
     constexpr int kRing = S::NG * S::NBUF * (F8 ? kF8Read : 2 * kBlock * D * 2);
     constexpr int kTarget = ((64 << 10) + kRing / 2) / kRing;
     return std::min(std::max(n, 1), std::max(kTarget, 1));
