@@ -1650,20 +1650,23 @@ mtn_status mtn_pool_set_linear(mtn_pool *P, const mtn_linear_config *cfg, void *
                 return fail(P, MTN_ERR_INVALID_ARG, "null, misaligned or small state buffer");
             if (!c.log_decay) return fail(P, MTN_ERR_INVALID_ARG, "null log_decay");
             const size_t n = (size_t)c.n_layers * c.n_kv_heads;
-            std::vector<float> powers(n * kLinDecays);
+            std::vector<float> powers(P->host_only ? 0 : n * kLinDecays);
             decays.resize(n + powers.size() / 2);
             for (size_t i = 0; i < n; ++i) {
                 if (!(c.log_decay[i] <= 0.f) || !std::isfinite(c.log_decay[i]))
                     return fail(P, MTN_ERR_INVALID_ARG, "log_decay above 0 or not finite");
                 decays[i] = c.log_decay[i] * 1.4426950408889634;
+                if (powers.empty()) continue;
                 float *const p = &powers[i * kLinDecays], *const rest = p + kLinTile + 1;
-                for (int m = 0; m <= kLinTile; ++m) {
-                    const double x = std::exp(m * (double)c.log_decay[i]);
+                // (64 products of 64 bits leave 57)
+                const long double lam = std::exp((long double)c.log_decay[i]);
+                long double x = 1.0L;
+                for (int m = 0; m <= kLinTile; ++m, x *= lam) {
                     p[m] = (float)x;
                     rest[m] = (float)(x - p[m]);
                 }
             }
-            std::memcpy(&decays[n], powers.data(), sizeof(float) * powers.size());
+            if (!powers.empty()) std::memcpy(&decays[n], powers.data(), sizeof(float) * powers.size());
             if (c.scale == 0.f) c.scale = (float)(1.0 / std::sqrt((double)c.head_dim));
         }
         c.log_decay = nullptr;

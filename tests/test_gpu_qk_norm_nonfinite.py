@@ -37,13 +37,11 @@ def _decode(pool, dtype, hq, hkv, d, rows, have, kind, fused, n_split):
 
 @pytest.mark.parametrize("n_split", [1, 3])
 @pytest.mark.parametrize("fused", [False, True])
-@pytest.mark.parametrize("kind", [1, 2])
-@pytest.mark.parametrize("dtype,g,d", [("bf16", 1, 64), ("bf16", 2, 128), ("bf16", 4, 64), ("bf16", 4, 128),
-                                       ("bf16", 8, 128), ("f32", 4, 128), ("f32", 1, 64)])
+@pytest.mark.parametrize("dtype,g,d,kind", [
+    *[("bf16", g, d, kind) for g, d in ((1, 64), (2, 128), (4, 64), (4, 128), (8, 128)) for kind in (1, 2)],
+    ("f32", 4, 128, 1), ("f32", 1, 64, 1)])
 def test_an_infinite_value_stays_infinite(dtype, g, d, kind, fused, n_split):
     """Every weight is above 0 (scores of normed rows lie within sqrt(d) of 0)."""
-    if dtype == "f32" and kind == 2:
-        pytest.skip("no matrix-core decode of fp32 pools")
     say(f"{dtype} G={g} D={d} kernel {kind} fused {fused} split {n_split}")
     hkv, have = 2, 90
     pool = make_pool(n_layers=1, hq=hkv * g, hkv=hkv, d=d, S=4, W=100, cmax=have, max_sessions=1, n_blocks=13,
