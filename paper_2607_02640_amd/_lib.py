@@ -355,11 +355,12 @@ class Pool:
         self.required_bytes, self.kv = n.value, kv
 
     def plan_begin(self, sids, n_tok, stream=None) -> None:
-        n_tok = _arr32(n_tok)
-        st = self.lib.mtn_plan_begin(self.h, len(sids), _arr32(sids), n_tok,
+        n_tok = [int(x) for x in n_tok]
+        st = self.lib.mtn_plan_begin(self.h, len(sids), _arr32(sids), (C.c_int32 * len(n_tok))(*n_tok),
                                      None if self.host_only else _stream(stream))
         self._check(st, "plan_begin")
-        self._plan_tokens = sum(n_tok[:len(sids)])
+        if self._linear_rows is not None:
+            self._plan_tokens = sum(n_tok[:len(sids)])
 
     def plan_commit(self) -> None:
         self._check(self.lib.mtn_plan_commit(self.h), "plan_commit")
